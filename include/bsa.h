@@ -54,8 +54,17 @@ enum bsa_status {
   BSA_ERR_DTYPE = -5,       /* shape.dtype is neither BSA_F32 nor BSA_BF16 */
   BSA_ERR_LAUNCH = -6,      /* the HIP runtime reported a launch error */
   BSA_ERR_WORKSPACE = -7,   /* workspace NULL or smaller than the *_workspace_bytes() figure */
-  BSA_ERR_STATIC_LIMIT = -8 /* bsa_select_kv_static: the shape needs more than BSA_STATIC_SELECT_BYTES */
+  BSA_ERR_STATIC_LIMIT = -8, /* bsa_select_kv_static: the shape needs more than BSA_STATIC_SELECT_BYTES */
+  BSA_ERR_STRIDE = -9       /* bsa_qk_norm_rope_*, bsa_cross_attn_*: a stride or address that is no multiple of 16
+                               bytes, a negative or huge stride, or an output whose elements would overlap */
 };
+
+/* Strides of a tensor with a batch, a token and a head index, in elements; the channels of a head are adjacent.
+ * Multiples of 16 bytes, 0 <= stride < 2^40; that of an extent of 1 counts for nothing.  Inputs may repeat (stride 0)
+ * or overlap, outputs may not. */
+typedef struct bsa_strides {
+  int64_t b, l, h;
+} bsa_strides_t;
 
 typedef struct bsa_shape {
   int32_t B, H;          /* batch, heads */
@@ -221,6 +230,98 @@ int bsa_dense_attn_fwd(const bsa_shape_t* shape, const void* Q, const void* K, c
 int bsa_dense_attn_bwd(const bsa_shape_t* shape, const void* Q, const void* K, const void* V,
                        const void* O, const float* LSE, const void* dO, float sm_scale,
                        void* dQ, void* dK, void* dV,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Per-head norm of queries and keys with the rotation by grid position in the same pass: what stands between a block's
+ * projections and its attention.  For every token n = (t, h, w) and head
+ *   Q = R(n) (wq * xq / sqrt(mean(xq^2) + eps)),  K likewise with xk and wk,  V = xv,
+ * where x is a head's d channels of the projection's output and R(n) turns pairs of channels (a, b) by an angle,
+ *   (a, b) -> (a cos - b sin, a sin + b cos),  angle = position * theta^(-2i/n_axis).
+ * Of the rope->dt + dh + dw rotated channels the first dt / 2 pairs turn with the token's t, the next dh / 2 with its h
+ * and the last dw / 2 with its w (i counts an axis's own pairs, n_axis is dt, dh or dw); the channels behind them are left
+ * as the norm gives them.  Arithmetic is fp32, each result is rounded once.  (A sum of squares beyond fp32, from
+ * elements of 1e18 on, makes a row zero.)
+ *   shape   B, H, T, Hs, Ws, d, dtype and layout; the block must divide the grid (1, 1, 1 will do for raster tensors),
+ *           Bk and N are not limited here; B*L < 2^31.  A text or any other sequence: T = length, Hs = Ws = 1.
+ *   rope    NULL: no rotation (table is not read either)
+ *   table   device, bsa_rope_table_bytes(): for t, then h, then w: [extent][n_axis / 2][2] = cos, sin of every
+ *           coordinate and pair.  bsa_rope_table() fills it; any other angles will do as well.
+ *   Xq, Xk, Xv   in  [B, L, H, d] shape.dtype, tokens in raster order, all of strides x: separate tensors or slices of a
+ *                    packed projection
+ *   wq, wk       in  [d] float, NULL: ones
+ *   Q, K, V      out [B, H, L, d] contiguous, token order of shape.layout: what the other calls take
+ * A tensor is left out by passing NULL for it and its result; at least one has to be there.
+ */
+enum bsa_rope_style {
+  BSA_ROPE_PAIRS = 0, /* pair i = channels (2i, 2i + 1) */
+  BSA_ROPE_HALVES = 1 /* pair i = channels (i, i + (dt + dh + dw) / 2) */
+};
+typedef struct bsa_rope {
+  int32_t dt, dh, dw; /* even, >= 0; the sum a multiple of 8 and at most d */
+  int32_t style;
+} bsa_rope_t;
+size_t bsa_rope_table_bytes(const bsa_shape_t* shape, const bsa_rope_t* rope);
+/* Fills table, angles in fp64: positions t0 + t, h0 + h, w0 + w (coordinates of the first token), 0 < theta < inf. */
+int bsa_rope_table(const bsa_shape_t* shape, const bsa_rope_t* rope, double theta, int64_t t0, int64_t h0, int64_t w0,
+                   float* table, void* stream);
+int bsa_qk_norm_rope_fwd(const bsa_shape_t* shape, const bsa_rope_t* rope, const float* table,
+                         const void* Xq, const void* Xk, const void* Xv, const bsa_strides_t* x,
+                         const float* wq, const float* wk, float eps /* > 0 */,
+                         void* Q, void* K, void* V, void* stream);
+
+/*
+ * Its backward: reads Xq and Xk again instead of anything the forward would have to keep.
+ *   dQ, dK, dV     in  [B, H, L, d] contiguous, token order of shape.layout
+ *   dXq, dXk, dXv  out [B, L, H, d] of strides dx
+ *   dwq, dwk       out [d] float, sums over batch, tokens and heads in a fixed order; NULL: not wanted
+ * Xq, dQ and dXq come together or not at all, so do Xk, dK and dXk, and dV and dXv.
+ *   workspace      bsa_qk_norm_rope_bwd_workspace_bytes(shape) bytes of device scratch
+ */
+size_t bsa_qk_norm_rope_bwd_workspace_bytes(const bsa_shape_t* shape);
+int bsa_qk_norm_rope_bwd(const bsa_shape_t* shape, const bsa_rope_t* rope, const float* table,
+                         const void* Xq, const void* Xk, const bsa_strides_t* x,
+                         const float* wq, const float* wk, float eps,
+                         const void* dQ, const void* dK, const void* dV,
+                         void* dXq, void* dXk, void* dXv, const bsa_strides_t* dx,
+                         float* dwq, float* dwk, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cross attention: the grid's tokens (or any queries) attend to S states of an encoder, dense softmax attention over the
+ * valid ones, O = softmax(sm_scale Q K^T) V.  Query head h reads key/value head h / (H / Hkv).
+ * State s of batch entry b is valid if s < kv_len[b] and kv_mask[b][s] is not 0.  What K and V hold at other states is
+ * never used, be it NaN.  A batch entry without a valid state gives O = 0 and LSE = -inf and has no gradients.
+ *   shape    1 <= Hkv, Hkv divides H; Lq, S >= 1, (H / Hkv) * Lq < 2^31; d a multiple of 8, at most 256
+ *   q, k, v, o   strides of Q, K, V, O
+ *   kv_len   device [B] int32, taken as 0 below 0 and as S above S; NULL: S for all
+ *   kv_mask  device [B][S] bytes; NULL: all 1
+ *   LSE      out [B, H, Lq] contiguous float, natural-log sum-exp
+ *   workspace  bsa_cross_attn_fwd_workspace_bytes(shape) bytes of device scratch (may be NULL when that is 0): partial
+ *              results where few query rows have their keys split over several workgroups
+ */
+typedef struct bsa_cross_shape {
+  int32_t B, H, Hkv;
+  int32_t Lq, S;
+  int32_t d, dtype;
+  bsa_strides_t q, k, v, o;
+} bsa_cross_shape_t;
+size_t bsa_cross_attn_fwd_workspace_bytes(const bsa_cross_shape_t* shape);
+int bsa_cross_attn_fwd(const bsa_cross_shape_t* shape, const void* Q, const void* K, const void* V,
+                       const int32_t* kv_len, const uint8_t* kv_mask, float sm_scale,
+                       void* O, float* LSE, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its backward.  dK and dV are sums over the query heads that share them, zero at states that are not valid; every
+ * element of dQ, dK and dV is written.  delta = <dO, O> uses the O the caller passes.
+ *   O, LSE   the forward's outputs
+ *   grads    host, strides of dO, dQ, dK, dV, in this order; NULL: those of O, Q, K, V
+ *   K and V that repeat (stride 0) have a gradient for every repetition, whose sum is the caller's.
+ */
+size_t bsa_cross_attn_bwd_workspace_bytes(const bsa_cross_shape_t* shape);
+int bsa_cross_attn_bwd(const bsa_cross_shape_t* shape, const void* Q, const void* K, const void* V,
+                       const void* O, const float* LSE, const void* dO,
+                       const int32_t* kv_len, const uint8_t* kv_mask, float sm_scale,
+                       void* dQ, void* dK, void* dV, const bsa_strides_t* grads,
                        void* workspace, size_t workspace_bytes, void* stream);
 
 /*

@@ -24,6 +24,8 @@ EXPORTS = (
     "bsa_strerror", "bsa_n_keep", "bsa_pool_blocks", "bsa_select_workspace_bytes", "bsa_select_kv",
     "bsa_select_kv_stat", "bsa_select_kv_static", "bsa_prune_q", "bsa_fwd_workspace_bytes", "bsa_attn_fwd", "bsa_bwd_workspace_bytes", "bsa_attn_bwd", "bsa_attn_bwd_stages",
     "bsa_dense_bwd_workspace_bytes", "bsa_dense_attn_fwd", "bsa_dense_attn_bwd", "bsa_mfma_probe",
+    "bsa_rope_table_bytes", "bsa_rope_table", "bsa_qk_norm_rope_fwd", "bsa_qk_norm_rope_bwd_workspace_bytes", "bsa_qk_norm_rope_bwd",
+    "bsa_cross_attn_fwd_workspace_bytes", "bsa_cross_attn_fwd", "bsa_cross_attn_bwd_workspace_bytes", "bsa_cross_attn_bwd",
 )
 
 
@@ -35,6 +37,18 @@ class BsaError(RuntimeError):
 
 class ShapeStruct(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("B", "H", "T", "Hs", "Ws", "Ct", "Ch", "Cw", "d", "dtype", "Wt", "Wh", "Ww", "layout")]
+
+
+class StridesStruct(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("b", "l", "h")]
+
+
+class RopeStruct(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dt", "dh", "dw", "style")]
+
+
+class CrossStruct(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "H", "Hkv", "Lq", "S", "d", "dtype")] + [(n, StridesStruct) for n in "qkvo"]
 
 
 _lib = None
@@ -73,6 +87,19 @@ def lib() -> C.CDLL:
         L.bsa_dense_attn_fwd.argtypes = [P, vp, vp, vp, f32, vp, vp, vp]
         L.bsa_dense_attn_bwd.restype = C.c_int
         L.bsa_dense_attn_bwd.argtypes = [P] + [vp] * 6 + [f32, vp, vp, vp, vp, sz, vp]
+        R, T, X = C.POINTER(RopeStruct), C.POINTER(StridesStruct), C.POINTER(CrossStruct)
+        L.bsa_rope_table_bytes.restype, L.bsa_rope_table_bytes.argtypes = sz, [P, R]
+        L.bsa_rope_table.restype, L.bsa_rope_table.argtypes = C.c_int, [P, R, f64, i64, i64, i64, vp, vp]
+        L.bsa_qk_norm_rope_fwd.restype = C.c_int
+        L.bsa_qk_norm_rope_fwd.argtypes = [P, R] + [vp] * 4 + [T, vp, vp, f32] + [vp] * 4
+        L.bsa_qk_norm_rope_bwd_workspace_bytes.restype, L.bsa_qk_norm_rope_bwd_workspace_bytes.argtypes = sz, [P]
+        L.bsa_qk_norm_rope_bwd.restype = C.c_int
+        L.bsa_qk_norm_rope_bwd.argtypes = [P, R] + [vp] * 3 + [T, vp, vp, f32] + [vp] * 6 + [T, vp, vp, vp, sz, vp]
+        L.bsa_cross_attn_fwd_workspace_bytes.restype, L.bsa_cross_attn_fwd_workspace_bytes.argtypes = sz, [X]
+        L.bsa_cross_attn_fwd.restype, L.bsa_cross_attn_fwd.argtypes = C.c_int, [X] + [vp] * 5 + [f32, vp, vp, vp, sz, vp]
+        L.bsa_cross_attn_bwd_workspace_bytes.restype, L.bsa_cross_attn_bwd_workspace_bytes.argtypes = sz, [X]
+        L.bsa_cross_attn_bwd.restype = C.c_int
+        L.bsa_cross_attn_bwd.argtypes = [X] + [vp] * 8 + [f32] + [vp] * 3 + [T, vp, sz, vp]
         L.bsa_mfma_probe.restype, L.bsa_mfma_probe.argtypes = i64, [i32, i32, vp, vp]
         _lib = L
     return _lib
@@ -295,6 +322,214 @@ def dense_attn_bwd(shape: Shape, Q, K, V, O, LSE, dO, sm_scale: Optional[float] 
     st = lib().bsa_dense_attn_bwd(C.byref(shape.c()), _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(LSE), _ptr(dO),
                                   sm_scale, _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(workspace), workspace.numel(), _stream())
     _check(st, "bsa_dense_attn_bwd")
+    return dQ, dK, dV
+
+
+# ---- the operators around the attention ----------------------------------------------------------
+# Their tensors may have any strides that the header allows, so each is checked here for what a pointer cannot tell.
+ROPE_PAIRS, ROPE_HALVES = 0, 1
+
+
+@dataclass(frozen=True)
+class Rope:
+    """Channels rotated by the grid's t, h and w coordinate, and how they pair up."""
+    dt: int
+    dh: int
+    dw: int
+    style: int = ROPE_PAIRS
+
+    def c(self) -> RopeStruct:
+        return RopeStruct(self.dt, self.dh, self.dw, self.style)
+
+
+@dataclass(frozen=True)
+class CrossShape:
+    B: int
+    H: int
+    Hkv: int
+    Lq: int
+    S: int
+    d: int
+    dtype: int  # F32 or BF16
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == F32 else torch.bfloat16
+
+    def c(self, Q=None, K=None, V=None, O=None) -> CrossStruct:
+        """With the strides of the given [B, heads, tokens, d] tensors (contiguous ones where there is none)."""
+        return CrossStruct(self.B, self.H, self.Hkv, self.Lq, self.S, self.d, self.dtype,
+                           *(_strides(t, 2, 1) if t is not None else StridesStruct(h * n * self.d, self.d, n * self.d)
+                             for t, h, n in ((Q, self.H, self.Lq), (K, self.Hkv, self.S), (V, self.Hkv, self.S), (O, self.H, self.Lq))))
+
+
+def _strides(t: torch.Tensor, l: int, h: int) -> StridesStruct:
+    """Of a tensor whose dimensions are batch, channels last and tokens and heads at l and h."""
+    s = t.stride()
+    return StridesStruct(s[0], s[l], s[h])
+
+
+def _device(t: torch.Tensor) -> torch.device:
+    """The device of a call: it has to be the current one, whose stream the work goes to."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors must be on the current GPU, not on {t.device}")
+    return t.device
+
+
+def _take(t: Optional[torch.Tensor], name: str, size, dtype, device, dense: bool = False) -> Optional[int]:
+    """The address of a tensor of that size, type and device, its last dimension (dense: all of it) contiguous; None for None."""
+    if t is None:
+        return None
+    if t.shape != size or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {tuple(size)} {dtype} on {device}, not {tuple(t.shape)} {t.dtype} on {t.device}")
+    if dense and not t.is_contiguous() or t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name} must be contiguous" if dense else f"{name}: the channels of a head must be adjacent")
+    return t.data_ptr()
+
+
+def _scratch(workspace: Optional[torch.Tensor], nbytes: int, device) -> Optional[torch.Tensor]:
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on {device}")
+    return workspace
+
+
+def rope_table(shape: Shape, rope: Rope, theta: float = 10000.0, origin=(0, 0, 0), out: Optional[torch.Tensor] = None,
+               device="cuda") -> torch.Tensor:
+    """cos and sin of every coordinate and pair; origin: coordinates of the grid's first token."""
+    nbytes = lib().bsa_rope_table_bytes(C.byref(shape.c()), C.byref(rope.c()))
+    if out is None:
+        out = torch.empty(max(1, nbytes // 4), dtype=torch.float32, device=device)
+    _device(out)
+    if out.dtype != torch.float32 or not out.is_contiguous() or out.numel() * 4 < nbytes:
+        raise ValueError(f"table must be {nbytes // 4} contiguous floats")
+    _check(lib().bsa_rope_table(C.byref(shape.c()), C.byref(rope.c()), theta, *origin, out.data_ptr(), _stream()), "bsa_rope_table")
+    return out
+
+
+def _rope_table_ptr(shape: Shape, rope: Optional[Rope], table: Optional[torch.Tensor], device) -> Optional[int]:
+    if rope is None or table is None or table.numel() == 0:
+        return None
+    need = lib().bsa_rope_table_bytes(C.byref(shape.c()), C.byref(rope.c())) // 4
+    if table.dtype != torch.float32 or table.device != device or not table.is_contiguous() or table.numel() < need:
+        raise ValueError(f"table must be {need} contiguous floats on {device}")
+    return table.data_ptr()
+
+
+def _same_strides(tensors, names):
+    """The common strides of the [B, L, H, d] tensors that are there (an extent of 1 has none)."""
+    there = [t for t in tensors if t is not None]
+    first = there[0]
+    for t in there[1:]:
+        if any(a != b and n > 1 for a, b, n in zip(t.stride(), first.stride(), first.shape)):
+            raise ValueError(f"{names} must have the same strides")
+    return C.byref(_strides(first, 1, 2))
+
+
+def qk_norm_rope_fwd(shape: Shape, rope: Optional[Rope], table: Optional[torch.Tensor], Xq=None, Xk=None, Xv=None,
+                     wq=None, wk=None, eps: float = 1e-6, Q=None, K=None, V=None):
+    """Xq, Xk, Xv: [B, L, H, d] of the same strides, None to leave one out.  Returns Q, K, V, [B, H, L, d] in the shape's order."""
+    X = (Xq, Xk, Xv)
+    if all(t is None for t in X):
+        raise ValueError("Xq, Xk or Xv must be given")
+    dev, dt = _device(next(t for t in X if t is not None)), shape.torch_dtype
+    size_in, size_out = (shape.B, shape.L, shape.H, shape.d), (shape.B, shape.H, shape.L, shape.d)
+    Y = [torch.empty(size_out, dtype=dt, device=dev) if x is not None and y is None else y for x, y in zip(X, (Q, K, V))]
+    args = [_take(x, n, size_in, dt, dev) for x, n in zip(X, ("Xq", "Xk", "Xv"))]
+    w = [_take(t, n, (shape.d,), torch.float32, dev, True) for t, n in ((wq, "wq"), (wk, "wk"))]
+    outs = [_take(y, n, size_out, dt, dev, True) for y, n in zip(Y, "QKV")]
+    rp = C.byref(rope.c()) if rope is not None else None
+    st = lib().bsa_qk_norm_rope_fwd(C.byref(shape.c()), rp, _rope_table_ptr(shape, rope, table, dev), *args,
+                                    _same_strides(X, "Xq, Xk and Xv"), *w, eps, *outs, _stream())
+    _check(st, "bsa_qk_norm_rope_fwd")
+    return tuple(Y)
+
+
+def qk_norm_rope_bwd_workspace_bytes(shape: Shape) -> int:
+    return lib().bsa_qk_norm_rope_bwd_workspace_bytes(C.byref(shape.c()))
+
+
+def qk_norm_rope_bwd(shape: Shape, rope: Optional[Rope], table: Optional[torch.Tensor], Xq=None, Xk=None, dQ=None, dK=None, dV=None,
+                     wq=None, wk=None, eps: float = 1e-6, dXq=None, dXk=None, dXv=None, dwq=None, dwk=None,
+                     workspace: Optional[torch.Tensor] = None):
+    """Returns dXq, dXk, dXv ([B, L, H, d], contiguous where not given, then all of the same strides), dwq, dwk ([d] float)."""
+    dY, X = (dQ, dK, dV), (Xq, Xk)
+    if all(t is None for t in dY):
+        raise ValueError("dQ, dK or dV must be given")
+    dev, dt = _device(next(t for t in dY if t is not None)), shape.torch_dtype
+    size_x, size_y = (shape.B, shape.L, shape.H, shape.d), (shape.B, shape.H, shape.L, shape.d)
+    dX = [torch.empty(size_x, dtype=dt, device=dev) if y is not None and x is None else x for y, x in zip(dY, (dXq, dXk, dXv))]
+    dw = [torch.empty(shape.d, dtype=torch.float32, device=dev) if y is not None and t is None else t for y, t in zip(dY, (dwq, dwk))]
+    xs = [_take(t, n, size_x, dt, dev) for t, n in zip(X, ("Xq", "Xk"))]
+    w = [_take(t, n, (shape.d,), torch.float32, dev, True) for t, n in ((wq, "wq"), (wk, "wk"))]
+    ys = [_take(t, n, size_y, dt, dev, True) for t, n in zip(dY, ("dQ", "dK", "dV"))]
+    outs = [_take(t, n, size_x, dt, dev) for t, n in zip(dX, ("dXq", "dXk", "dXv"))]
+    dws = [_take(t, n, (shape.d,), torch.float32, dev, True) for t, n in zip(dw, ("dwq", "dwk"))]
+    workspace = _scratch(workspace, qk_norm_rope_bwd_workspace_bytes(shape), dev)
+    rp = C.byref(rope.c()) if rope is not None else None
+    st = lib().bsa_qk_norm_rope_bwd(C.byref(shape.c()), rp, _rope_table_ptr(shape, rope, table, dev), *xs,
+                                    _same_strides(X, "Xq and Xk") if any(t is not None for t in X) else None, *w, eps, *ys, *outs,
+                                    _same_strides(dX, "dXq, dXk and dXv"), *dws, _ptr(workspace),
+                                    workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    _check(st, "bsa_qk_norm_rope_bwd")
+    return (*dX, *dw)
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """Memory for a tensor like t, in t's order of dimensions, without its repetitions."""
+    return torch.empty_like(t) if all(s > 0 for s, n in zip(t.stride(), t.shape) if n > 1) else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def cross_fwd_workspace_bytes(shape: CrossShape) -> int:
+    return lib().bsa_cross_attn_fwd_workspace_bytes(C.byref(shape.c()))
+
+
+def cross_bwd_workspace_bytes(shape: CrossShape) -> int:
+    return lib().bsa_cross_attn_bwd_workspace_bytes(C.byref(shape.c()))
+
+
+def cross_attn_fwd(shape: CrossShape, Q, K, V, kv_len: Optional[torch.Tensor] = None, kv_mask: Optional[torch.Tensor] = None,
+                   sm_scale: Optional[float] = None, O=None, LSE=None, workspace: Optional[torch.Tensor] = None):
+    """Q: [B, H, Lq, d]; K, V: [B, Hkv, S, d]; any strides with adjacent channels.  kv_len: [B] int32; kv_mask: [B, S] uint8 or bool."""
+    dev, dt = _device(Q), shape.torch_dtype
+    O = _like(Q) if O is None else O
+    LSE = torch.empty((shape.B, shape.H, shape.Lq), dtype=torch.float32, device=dev) if LSE is None else LSE
+    qs, ks = (shape.B, shape.H, shape.Lq, shape.d), (shape.B, shape.Hkv, shape.S, shape.d)
+    ins = [_take(t, n, s, dt, dev) for t, n, s in ((Q, "Q", qs), (K, "K", ks), (V, "V", ks))]
+    valid = _valid(shape, kv_len, kv_mask, dev)
+    outs = [_take(O, "O", qs, dt, dev), _take(LSE, "LSE", qs[:3], torch.float32, dev, True)]
+    c = shape.c(Q, K, V, O)
+    workspace = _scratch(workspace, lib().bsa_cross_attn_fwd_workspace_bytes(C.byref(c)), dev)
+    st = lib().bsa_cross_attn_fwd(C.byref(c), *ins, *valid, 1.0 / sqrt(shape.d) if sm_scale is None else sm_scale, *outs, _ptr(workspace),
+                                  workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    _check(st, "bsa_cross_attn_fwd")
+    return O, LSE
+
+
+def _valid(shape: CrossShape, kv_len, kv_mask, dev):
+    if kv_mask is not None and kv_mask.dtype == torch.bool:
+        kv_mask = kv_mask.view(torch.uint8)
+    return (_take(kv_len, "kv_len", (shape.B,), torch.int32, dev, True),
+            _take(kv_mask, "kv_mask", (shape.B, shape.S), torch.uint8, dev, True))
+
+
+def cross_attn_bwd(shape: CrossShape, Q, K, V, O, LSE, dO, kv_len: Optional[torch.Tensor] = None, kv_mask: Optional[torch.Tensor] = None,
+                   sm_scale: Optional[float] = None, dQ=None, dK=None, dV=None, workspace: Optional[torch.Tensor] = None):
+    """dO, dQ, dK, dV may have strides of their own.  Of K and V that repeat (expanded), dK and dV hold every repetition's gradient."""
+    dev, dt = _device(Q), shape.torch_dtype
+    dQ, dK, dV = (_like(t) if g is None else g for t, g in ((Q, dQ), (K, dK), (V, dV)))
+    qs, ks = (shape.B, shape.H, shape.Lq, shape.d), (shape.B, shape.Hkv, shape.S, shape.d)
+    ins = [_take(t, n, s, dt, dev) for t, n, s in ((Q, "Q", qs), (K, "K", ks), (V, "V", ks), (O, "O", qs))]
+    ins += [_take(LSE, "LSE", qs[:3], torch.float32, dev, True), _take(dO, "dO", qs, dt, dev)]
+    valid = _valid(shape, kv_len, kv_mask, dev)
+    outs = [_take(t, n, s, dt, dev) for t, n, s in ((dQ, "dQ", qs), (dK, "dK", ks), (dV, "dV", ks))]
+    c = shape.c(Q, K, V, O)
+    grads = (StridesStruct * 4)(*(_strides(t, 2, 1) for t in (dO, dQ, dK, dV)))
+    workspace = _scratch(workspace, lib().bsa_cross_attn_bwd_workspace_bytes(C.byref(c)), dev)
+    st = lib().bsa_cross_attn_bwd(C.byref(c), *ins, *valid, 1.0 / sqrt(shape.d) if sm_scale is None else sm_scale, *outs, grads,
+                                  _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+    _check(st, "bsa_cross_attn_bwd")
     return dQ, dK, dV
 
 

@@ -20,6 +20,8 @@ SOURCES = [
     "bsa_attn_fwd.hip",
     "bsa_attn_pipe.hip",
     "bsa_attn_dkv.hip",
+    "bsa_qk_norm_rope.hip",
+    "bsa_cross.hip",
     "bsa_probe.hip",
 ]
 # -ffp-contract=off: the decision kernels fix every rounding; packed-fp32 ops are disabled

@@ -73,6 +73,7 @@ __host__ __device__ inline int window_center(const Geom& g, int w) {
 __host__ __device__ inline int center_of(const Geom& g, int c) { return window_center(g, window_of(g, c)); }
 
 int make_geom(const bsa_shape_t* s, Geom* g);  // validates; returns bsa_status
+int make_token_geom(const bsa_shape_t* s, Geom* g);  // the same without the limits on Bk, N and rows, for calls that only move tokens
 
 inline int check_launch() {
   return hipGetLastError() == hipSuccess ? BSA_OK : BSA_ERR_LAUNCH;
@@ -155,5 +156,43 @@ int launch_fwd_pipe(const Geom& g, const AttnArgs& a, hipStream_t st);
 int launch_bwd_pipe(const Geom& g, const AttnArgs& a, hipStream_t st);
 size_t bwd_workspace_pipe(const Geom& g, int n_keep);
 size_t fwd_workspace_pipe(const Geom& g, int n_keep);
+
+// ---- bsa_qk_norm_rope_*: index 0, 1, 2 = queries, keys, values; a missing tensor has null pointers ----
+struct RopeArgs {
+  const void* X[3];  // [B, L, H, d], strides x
+  void* Y[3];        // [B, H, L, d] (forward: out)
+  const void* dY[3];
+  void* dX[3];       // strides dx
+  const float* w[2];
+  float* dw[2];
+  bsa_strides_t x, dx;
+  const float* table;
+  int nt, nh, nw;    // pairs of each axis; all 0: no rotation
+  int halves;
+  float eps;
+  float* part;       // backward: partial sums of dw
+};
+int launch_rope_table(const Geom& g, const RopeArgs& a, double theta, const double origin[3], float* table, hipStream_t st);
+int launch_rope_fwd(const Geom& g, int dtype, const RopeArgs& a, hipStream_t st);
+int launch_rope_bwd(const Geom& g, int dtype, const RopeArgs& a, hipStream_t st);
+size_t rope_bwd_workspace(const Geom& g);
+
+// ---- bsa_cross_attn_* ----
+struct CrossArgs {
+  const void *Q, *K, *V, *O, *dO;
+  const float* LSE_in;
+  const int32_t* kv_len;
+  const uint8_t* kv_mask;
+  void *O_out, *dQ, *dK, *dV;
+  float* LSE_out;
+  int B, H, Hkv, G, Lq, M, S, d, dtype;  // G = H / Hkv heads share keys; their M = G * Lq query rows are one after the other
+  bsa_strides_t q, k, v, o, go, gq, gk, gv;
+  float sm_scale;
+  void* ws;
+};
+size_t cross_fwd_workspace(const CrossArgs& a);
+size_t cross_bwd_workspace(const CrossArgs& a);
+int launch_cross_fwd(const CrossArgs& a, hipStream_t st);
+int launch_cross_bwd(const CrossArgs& a, hipStream_t st);
 
 }  // namespace bsa

@@ -1,0 +1,397 @@
+// Per-head RMS norm of queries and keys and their rotation by grid position, from the projection's output [B, L, H, d] to the
+// attention's [B, H, L, d] (raster or block-major), values moved along; and the backward.
+//
+//   xhat = x r, r = 1 / sqrt(mean(x^2) + eps);  y = R (w xhat)
+//   u = R^T dy;  dw = sum u xhat;  g = w u;  dx = r (g - xhat mean(g xhat))
+//
+// What bounds it: memory.  Every element is read once and written once (backward: x and dy read, dx written), some ten
+// operations each.  A row (the d channels of a head's token) lies in 2^k lanes, eight channels each, so a wavefront holds
+// 64 / 2^k rows: consecutive tokens of the result, whose writes are one run.  A lane keeps its tokens' cosines and sines in
+// registers for all heads and tensors, and the row sums are register exchanges.
+#include "bsa_common.h"
+
+namespace bsa {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+// ---- eight channels of a lane, in two pieces of four at p + o0 and p + o1 (elements) ----
+template <bool SPLIT>
+__device__ inline void load8(const uint16_t* p, int o0, int o1, float x[8]) {
+  u32x4 v;
+  if (SPLIT) {
+    const u32x2 a = *reinterpret_cast<const u32x2*>(p + o0), b = *reinterpret_cast<const u32x2*>(p + o1);
+    v = u32x4{a.x, a.y, b.x, b.y};
+  } else {
+    v = *reinterpret_cast<const u32x4*>(p + o0);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(v[i] << 16);
+    x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+  }
+}
+template <bool SPLIT>
+__device__ inline void load8(const float* p, int o0, int o1, float x[8]) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p + o0), b = *reinterpret_cast<const f32x4*>(p + o1);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = a[i];
+    x[4 + i] = b[i];
+  }
+}
+__device__ inline uint32_t pack2(float lo, float hi) {
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  const f32x2 v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+template <bool SPLIT>
+__device__ inline void store8(uint16_t* p, int o0, int o1, const float x[8]) {
+  const u32x4 v = {pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+  if (SPLIT) {
+    *reinterpret_cast<u32x2*>(p + o0) = u32x2{v.x, v.y};
+    *reinterpret_cast<u32x2*>(p + o1) = u32x2{v.z, v.w};
+  } else {
+    *reinterpret_cast<u32x4*>(p + o0) = v;
+  }
+}
+template <bool SPLIT>
+__device__ inline void store8(float* p, int o0, int o1, const float x[8]) {
+  *reinterpret_cast<f32x4*>(p + o0) = f32x4{x[0], x[1], x[2], x[3]};
+  *reinterpret_cast<f32x4*>(p + o1) = f32x4{x[4], x[5], x[6], x[7]};
+}
+
+// Sum over the LPR lanes of a row, the same value in all of them: lane exchanges by data-parallel primitives.
+template <int CTRL>
+__device__ inline float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int LPR>
+__device__ inline float row_sum(float v) {
+  v = dpp_add<0xB1>(v);                       // lane ^ 1
+  v = dpp_add<0x4E>(v);                       // lane ^ 2
+  if (LPR >= 8) v = dpp_add<0x141>(v);        // mirrored within 8: the other four
+  if (LPR >= 16) v = dpp_add<0x140>(v);       // mirrored within 16: the other eight
+  if (LPR >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return v;
+}
+
+// What a lane knows of its place: which channels, and how they turn.
+template <int LPR, bool HALVES>
+struct Place {
+  int c, o0, o1, rows_at;
+  bool live, turns;
+  int pair[4], axis;  // of the lane's four pairs: number on its axis; axes, two bits each
+
+  __device__ inline Place(const Geom& g, const RopeArgs& a, int lane) {
+    c = lane & (LPR - 1);
+    rows_at = lane / LPR;
+    live = 8 * c < g.d;
+    const int np = a.nt + a.nh + a.nw;
+    turns = live && 4 * c < np;
+    o0 = live ? 8 * c : 0;  // (lanes past d take part in the sums, with nothing)
+    o1 = o0 + 4;
+    if (HALVES && turns) {
+      o0 = 4 * c;
+      o1 = np + o0;
+    }
+    axis = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = 4 * c + i, x = p < a.nt ? 0 : p < a.nt + a.nh ? 1 : 2;
+      axis |= x << (2 * i);
+      pair[i] = p - (x == 0 ? 0 : x == 1 ? a.nt : a.nt + a.nh);
+    }
+  }
+  // cosines and sines of raster token n (unturned: 1, 0)
+  __device__ inline void angles(const Geom& g, const RopeArgs& a, int n, float cs[4], float sn[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
+    if (!turns) return;
+    const int w = n % g.Ws, th = n / g.Ws, h = th % g.Hs, t = th / g.Hs;
+    const int64_t at[3] = {(int64_t)t * a.nt, (int64_t)g.T * a.nt + (int64_t)h * a.nh,
+                           (int64_t)g.T * a.nt + (int64_t)g.Hs * a.nh + (int64_t)w * a.nw};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = (axis >> (2 * i)) & 3;
+      const float2 v = reinterpret_cast<const float2*>(a.table)[(x == 0 ? at[0] : x == 1 ? at[1] : at[2]) + pair[i]];
+      cs[i] = v.x;
+      sn[i] = v.y;
+    }
+  }
+};
+
+template <bool HALVES>
+__device__ inline void turn(float x[8], const float cs[4], const float sn[4], float sign) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int lo = HALVES ? i : 2 * i, hi = HALVES ? 4 + i : 2 * i + 1;
+    const float u = x[lo], v = x[hi], s = sign * sn[i];
+    x[lo] = __builtin_fmaf(u, cs[i], -(v * s));
+    x[hi] = __builtin_fmaf(u, s, v * cs[i]);
+  }
+}
+
+// Raster token of row m of a result in the shape's order.
+__device__ inline int raster_token(const Geom& g, int m) {
+  if (!g.tiled) return m;
+  const int i = m / g.Bk, k = m - i * g.Bk;
+  const int bw = i % g.Nw, bh = (i / g.Nw) % g.Nh, bt = i / (g.Nw * g.Nh);
+  const int cw = k % g.Cw, ch = (k / g.Cw) % g.Ch, ct = k / (g.Cw * g.Ch);
+  return ((bt * g.Ct + ct) * g.Hs + (bh * g.Ch + ch)) * g.Ws + (bw * g.Cw + cw);
+}
+
+template <typename T, int LPR, bool HALVES>
+__global__ __launch_bounds__(256) void rope_fwd_kernel(Geom g, RopeArgs a, int heads) {
+  constexpr int RPW = 64 / LPR, HB = 4;  // rows of a wavefront, heads in flight
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Place<LPR, HALVES> pl(g, a, lane);
+  const int64_t at = ((int64_t)blockIdx.x * 4 + wave) * RPW + pl.rows_at;  // row of the results, over the batch
+  if (at >= (int64_t)g.B * g.L) return;                                   // (a row's lanes leave together)
+  const int b = (int)(at / g.L), m = (int)(at - (int64_t)b * g.L), n = raster_token(g, m);
+  const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, g.H);
+  float cs[4], sn[4];
+  pl.angles(g, a, n, cs, sn);
+  const int64_t from = b * a.x.b + n * a.x.l, to = ((int64_t)b * g.H * g.L + m) * g.d;
+  const float inv_d = 1.f / g.d;
+#pragma unroll
+  for (int z = 0; z < 2; ++z) {
+    if (!a.X[z]) continue;
+    const T* X = static_cast<const T*>(a.X[z]) + from;
+    T* Y = static_cast<T*>(a.Y[z]) + to;
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = a.w[z] ? a.w[z][(i < 4 ? pl.o0 : pl.o1 - 4) + i] : 1.f;
+    for (int h = h0; h < h1; h += HB) {
+      float x[HB][8];
+#pragma unroll
+      for (int j = 0; j < HB; ++j) load8<HALVES>(X + min(h + j, h1 - 1) * a.x.h, pl.o0, pl.o1, x[j]);
+#pragma unroll
+      for (int j = 0; j < HB; ++j) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[j][i], x[j][i], s);
+        const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<LPR>(pl.live ? s : 0.f), inv_d, a.eps));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] = x[j][i] * r * w[i];
+        if (pl.turns) turn<HALVES>(x[j], cs, sn, 1.f);
+        if (pl.live && h + j < h1) store8<HALVES>(Y + (int64_t)(h + j) * g.L * g.d, pl.o0, pl.o1, x[j]);
+      }
+    }
+  }
+  if (a.X[2] && pl.live) {
+    const T* X = static_cast<const T*>(a.X[2]) + from + 8 * pl.c;
+    T* Y = static_cast<T*>(a.Y[2]) + to + 8 * pl.c;
+    constexpr int NV = sizeof(T) * 8 / 16;
+#pragma unroll 4
+    for (int h = h0; h < h1; ++h)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        reinterpret_cast<u32x4*>(Y + (int64_t)h * g.L * g.d)[i] = reinterpret_cast<const u32x4*>(X + h * a.x.h)[i];
+  }
+}
+
+// Backward.  A workgroup takes groups of rows in turn and keeps its share of dw in registers; the workgroups' sums are added
+// up by a second launch, in a fixed order.
+template <typename T, int LPR, bool HALVES>
+__global__ __launch_bounds__(256) void rope_bwd_kernel(Geom g, RopeArgs a, int heads) {
+  constexpr int RPW = 64 / LPR, HB = 2;
+  __shared__ float red[4][64][8];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Place<LPR, HALVES> pl(g, a, lane);
+  const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, g.H);
+  const float inv_d = 1.f / g.d;
+  float dw[2][8], w[2][8];
+#pragma unroll
+  for (int z = 0; z < 2; ++z)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      dw[z][i] = 0.f;
+      w[z][i] = a.w[z] ? a.w[z][(i < 4 ? pl.o0 : pl.o1 - 4) + i] : 1.f;
+    }
+  const int64_t rows = (int64_t)g.B * g.L;
+  for (int64_t first = ((int64_t)blockIdx.x * 4 + wave) * RPW; first < rows; first += (int64_t)gridDim.x * 4 * RPW) {
+    const int64_t at = first + pl.rows_at;
+    if (at >= rows) continue;
+    const int b = (int)(at / g.L), m = (int)(at - (int64_t)b * g.L), n = raster_token(g, m);
+    float cs[4], sn[4];
+    pl.angles(g, a, n, cs, sn);
+    const int64_t from = b * a.x.b + n * a.x.l, back = b * a.dx.b + n * a.dx.l, to = ((int64_t)b * g.H * g.L + m) * g.d;
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      if (!a.X[z]) continue;
+      const T* X = static_cast<const T*>(a.X[z]) + from;
+      const T* dY = static_cast<const T*>(a.dY[z]) + to;
+      T* dX = static_cast<T*>(a.dX[z]) + back;
+      for (int h = h0; h < h1; h += HB) {
+        float x[HB][8], u[HB][8];
+#pragma unroll
+        for (int j = 0; j < HB; ++j) {
+          load8<HALVES>(X + min(h + j, h1 - 1) * a.x.h, pl.o0, pl.o1, x[j]);
+          load8<HALVES>(dY + (int64_t)min(h + j, h1 - 1) * g.L * g.d, pl.o0, pl.o1, u[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < HB; ++j) {
+          if (pl.turns) turn<HALVES>(u[j], cs, sn, -1.f);
+          const bool there = pl.live && h + j < h1;
+          float s = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[j][i], x[j][i], s);
+          const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<LPR>(pl.live ? s : 0.f), inv_d, a.eps));
+          float t = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[j][i] *= r;
+            if (there) dw[z][i] = __builtin_fmaf(u[j][i], x[j][i], dw[z][i]);
+            u[j][i] *= w[z][i];
+            t = __builtin_fmaf(u[j][i], x[j][i], t);
+          }
+          t = row_sum<LPR>(pl.live ? t : 0.f) * inv_d;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[j][i] = r * __builtin_fmaf(-x[j][i], t, u[j][i]);
+          if (there) store8<HALVES>(dX + (h + j) * a.dx.h, pl.o0, pl.o1, u[j]);
+        }
+      }
+    }
+    if (a.dY[2] && pl.live) {
+      const T* dY = static_cast<const T*>(a.dY[2]) + to + 8 * pl.c;
+      T* dX = static_cast<T*>(a.dX[2]) + back + 8 * pl.c;
+      constexpr int NV = sizeof(T) * 8 / 16;
+#pragma unroll 4
+      for (int h = h0; h < h1; ++h)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          reinterpret_cast<u32x4*>(dX + h * a.dx.h)[i] = reinterpret_cast<const u32x4*>(dY + (int64_t)h * g.L * g.d)[i];
+    }
+  }
+  // the workgroup's sums: its 4 * RPW row slots in a fixed order
+#pragma unroll
+  for (int z = 0; z < 2; ++z) {
+    if (!a.dw[z]) continue;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) red[wave][lane][i] = dw[z][i];
+    __syncthreads();
+    if (threadIdx.x < LPR && pl.live) {
+      const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+      float* out = a.part + (wg * 2 + z) * g.d;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float s = 0.f;
+        for (int v = 0; v < 4; ++v)
+          for (int k = 0; k < RPW; ++k) s += red[v][k * LPR + lane][i];
+        out[(i < 4 ? pl.o0 : pl.o1 - 4) + i] = s;
+      }
+    }
+  }
+}
+
+// dw: sums over the workgroups' shares, fp64.  16 channels and 16 shares a workgroup at a time.
+__global__ __launch_bounds__(256) void rope_dw_kernel(const float* part, int n, int d, float* dwq, float* dwk) {
+  __shared__ double red[16][16];
+  float* out = blockIdx.y ? dwk : dwq;
+  if (!out) return;
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), k = threadIdx.x >> 4;
+  double s = 0.;
+  if (c < d)
+#pragma unroll 8
+    for (int i = k; i < n; i += 16) s += part[((int64_t)i * 2 + blockIdx.y) * d + c];
+  red[k][threadIdx.x & 15] = s;
+  __syncthreads();
+  if (k == 0 && c < d) {
+    for (int i = 1; i < 16; ++i) s += red[i][threadIdx.x & 15];
+    out[c] = (float)s;
+  }
+}
+
+__global__ __launch_bounds__(256) void rope_table_kernel(Geom g, int nt, int nh, int nw, double log_theta, double t0, double h0,
+                                                         double w0, float2* table) {
+  const int64_t a = (int64_t)g.T * nt, b = a + (int64_t)g.Hs * nh, all = b + (int64_t)g.Ws * nw;
+  for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < all; k += (int64_t)gridDim.x * 256) {
+    const int n = k < a ? nt : k < b ? nh : nw;
+    const int64_t at = k - (k < a ? 0 : k < b ? a : b);
+    const double pos = (k < a ? t0 : k < b ? h0 : w0) + (double)(at / n);
+    const double angle = pos * exp(-log_theta * (double)(at % n) / n);
+    table[k] = make_float2((float)cos(angle), (float)sin(angle));
+  }
+}
+
+constexpr int kBwdGroups = 2048;  // workgroups of a backward launch at most (two a SIMD): each leaves 2 d sums
+
+// Heads of a workgroup and workgroups along them: all heads, unless that leaves the chip short of wavefronts.
+static int head_split(int64_t groups, int H) {
+  const int64_t want = (1024 + groups - 1) / groups;
+  const int parts = (int)(want < 1 ? 1 : want > H ? H : want);
+  return (H + parts - 1) / parts;
+}
+
+static int lanes_of(int d) { return d <= 32 ? 4 : d <= 64 ? 8 : d <= 128 ? 16 : 32; }
+
+static dim3 bwd_grid(const Geom& g, int* heads) {
+  const int rpw = 64 / lanes_of(g.d);
+  const int64_t groups = ((int64_t)g.B * g.L + 4 * rpw - 1) / (4 * rpw);
+  *heads = head_split(groups, g.H);
+  const int parts = (g.H + *heads - 1) / *heads;
+  const int64_t most = kBwdGroups / parts;  // (head_split leaves parts > 1 only where groups * parts is about 1024)
+  return dim3((unsigned)(groups < most ? groups : most < 1 ? 1 : most), parts);
+}
+
+size_t rope_bwd_workspace(const Geom& g) {
+  int heads;
+  const dim3 n = bwd_grid(g, &heads);
+  return (size_t)n.x * n.y * 2 * g.d * sizeof(float);
+}
+
+template <typename T, int LPR, bool HALVES>
+static int launch_t(const Geom& g, const RopeArgs& a, bool backward, hipStream_t st) {
+  int heads;
+  if (backward) {
+    const dim3 grid = bwd_grid(g, &heads);
+    hipLaunchKernelGGL((rope_bwd_kernel<T, LPR, HALVES>), grid, dim3(256), 0, st, g, a, heads);
+    if (const int rc = check_launch()) return rc;
+    if (a.dw[0] || a.dw[1]) {
+      hipLaunchKernelGGL(rope_dw_kernel, dim3((g.d + 15) / 16, 2), dim3(256), 0, st, a.part, (int)(grid.x * grid.y), g.d, a.dw[0], a.dw[1]);
+      return check_launch();
+    }
+    return BSA_OK;
+  }
+  constexpr int RPW = 64 / LPR;
+  const int64_t groups = ((int64_t)g.B * g.L + 4 * RPW - 1) / (4 * RPW);
+  heads = head_split(groups, g.H);
+  hipLaunchKernelGGL((rope_fwd_kernel<T, LPR, HALVES>), dim3((unsigned)groups, (g.H + heads - 1) / heads), dim3(256), 0, st, g, a, heads);
+  return check_launch();
+}
+
+template <typename T>
+static int launch(const Geom& g, const RopeArgs& a, bool backward, hipStream_t st) {
+  switch (lanes_of(g.d)) {
+    case 4: return a.halves ? launch_t<T, 4, true>(g, a, backward, st) : launch_t<T, 4, false>(g, a, backward, st);
+    case 8: return a.halves ? launch_t<T, 8, true>(g, a, backward, st) : launch_t<T, 8, false>(g, a, backward, st);
+    case 16: return a.halves ? launch_t<T, 16, true>(g, a, backward, st) : launch_t<T, 16, false>(g, a, backward, st);
+    default: return a.halves ? launch_t<T, 32, true>(g, a, backward, st) : launch_t<T, 32, false>(g, a, backward, st);
+  }
+}
+
+int launch_rope_fwd(const Geom& g, int dtype, const RopeArgs& a, hipStream_t st) {
+  return dtype == BSA_F32 ? launch<float>(g, a, false, st) : launch<uint16_t>(g, a, false, st);
+}
+
+int launch_rope_bwd(const Geom& g, int dtype, const RopeArgs& a, hipStream_t st) {
+  return dtype == BSA_F32 ? launch<float>(g, a, true, st) : launch<uint16_t>(g, a, true, st);
+}
+
+int launch_rope_table(const Geom& g, const RopeArgs& a, double theta, const double origin[3], float* table, hipStream_t st) {
+  const int64_t n = (int64_t)g.T * a.nt + (int64_t)g.Hs * a.nh + (int64_t)g.Ws * a.nw;
+  if (n == 0) return BSA_OK;
+  const int64_t grid = (n + 255) / 256;
+  hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)(grid < 4096 ? grid : 4096)), dim3(256), 0, st, g, a.nt, a.nh, a.nw, log(theta),
+                     origin[0], origin[1], origin[2], reinterpret_cast<float2*>(table));
+  return check_launch();
+}
+
+}  // namespace bsa
