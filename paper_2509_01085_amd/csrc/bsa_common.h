@@ -188,6 +188,7 @@ struct CrossArgs {
   int B, H, Hkv, G, Lq, M, S, d, dtype;  // G = H / Hkv heads share keys; their M = G * Lq query rows are one after the other
   bsa_strides_t q, k, v, o, go, gq, gk, gv;
   float sm_scale;
+  int near;  // 64 rows of every tensor that is streamed lie within 2^31 bytes
   void* ws;
 };
 size_t cross_fwd_workspace(const CrossArgs& a);

@@ -11,6 +11,21 @@
 
 namespace bsa {
 
+// The arguments of a call where the kernel finds them: a piece of work loads what it needs from there.  By value, all of them would sit
+// in scalar registers for the whole kernel, or in lanes of vector registers when those run out.
+using Args = const __attribute__((address_space(4))) CrossArgs;
+__device__ inline Args* kernel_args() {
+#ifdef __HIP_DEVICE_COMPILE__
+  return (Args*)__builtin_amdgcn_kernarg_segment_ptr();  // CrossArgs is every kernel's first argument
+#else
+  return nullptr;
+#endif
+}
+__device__ inline Args* afresh(Args* a) {
+  asm volatile("" : "+s"(a));
+  return a;
+}
+
 // ---- element types ----
 template <typename T> struct Elt;
 template <> struct Elt<uint16_t> {
@@ -87,10 +102,12 @@ struct TileView {
       return {lds_frag_tr(p0, p1)};
     } else {
       typename E::Frag8 f;
-      const int ch = 32 * dt + (lane & 31);
+      int own = lane;  // (not known to the compiler: eight addresses a channel tile, held over the walk, would fill the registers)
+      asm volatile("" : "+v"(own));
+      const int ch = 32 * dt + (own & 31);
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const int r = row0 + 8 * (t >> 2) + 4 * grp + (t & 3);
+        const int r = row0 + 8 * (t >> 2) + 4 * (own >> 5) + (t & 3);
         f.v[t] = *reinterpret_cast<const float*>(tile + r * RB + (((ch >> 2) ^ tile_swz<T, DP>(r)) << 4) + 4 * (ch & 3));
       }
       return f;
@@ -101,32 +118,64 @@ struct TileView {
 // What rows and channels that do not exist read instead.
 __device__ __constant__ const uint4 kZeroChunk = {0, 0, 0, 0};
 
-// Requests a tile of ROWS rows from a tensor whose row r starts at base + r * stride (elements); rows whose bit in `there` is
-// not set, and channels from d on, arrive as zeros.  All NT threads of the workgroup take part; counted by vmcnt.
+// Requests tiles of ROWS rows from a tensor whose row r starts at base + r * stride (elements).  All NT threads of the workgroup
+// take part; counted by vmcnt.  Chunks from channel d on are never requested: clear() zeroes them once.
 template <typename T, int DP, int ROWS, int NT>
-__device__ inline void request_tile(uint8_t* tile, const T* base, int64_t stride, uint64_t there, int d, int tid) {
+struct Requests {
   using V = TileView<T, DP>;
-  constexpr int CHUNKS = ROWS * V::CPR;
-  static_assert(CHUNKS % NT == 0, "whole requests");
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  static constexpr int N = ROWS * V::CPR / NT;  // requests of a thread
+  static_assert(ROWS * V::CPR % NT == 0, "whole requests");
+  uint32_t off[N];  // byte offsets from the tile's first row; not used unless they fit (near)
+  int tid, d;
+  __device__ inline int row(int n) const { return (n * NT + tid) / V::CPR; }
+  __device__ inline int channel(int n) const { return (((n * NT + tid) % V::CPR) ^ tile_swz<T, DP>(row(n))) * V::E::CE; }
+  __device__ inline Requests(int64_t stride, int d_, int tid_) : tid(tid_), d(d_) {
 #pragma unroll
-  for (int n = 0; n < CHUNKS / NT; ++n) {
-    const int i = n * NT + tid, r = i / V::CPR, c = (i % V::CPR) ^ tile_swz<T, DP>(r);
-    const void* src = ((there >> r) & 1) && c * V::E::CE < d ? (const void*)(base + r * stride + c * V::E::CE) : (const void*)&kZeroChunk;
-    dma16(src, tile + (n * NT + wave * 64) * 16);
+    for (int n = 0; n < N; ++n) off[n] = (uint32_t)((row(n) * stride + channel(n)) * (int64_t)sizeof(T));
   }
-}
+  __device__ inline void clear(uint8_t* tile) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (channel(n) >= d) *reinterpret_cast<u32x4*>(tile + (n * NT + tid) * 16) = u32x4{0, 0, 0, 0};
+  }
+  // All rows of the tile are there and offsets fit: no arithmetic for a lane.
+  __device__ inline void whole(uint8_t* tile, const T* base) const {
+    const uint64_t sbase = uniform64(base);
+    const uint32_t lds = uniform_lds(tile + (tid >> 6) * 1024);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (channel(n) < d) dma16_raw(sbase, off[n], lds + n * NT * 16);
+  }
+  // Rows whose bit in `there` is not set arrive as zeros.
+  __device__ inline void some(uint8_t* tile, const T* base, int64_t stride, uint64_t there) const {
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+#pragma unroll 1
+    for (int n = 0; n < N; ++n) {
+      const int r = row(n), ch = channel(n);
+      const void* src = ((there >> r) & 1) && ch < d ? (const void*)(base + r * stride + ch) : (const void*)&kZeroChunk;
+      dma16(src, tile + (n * NT + wave * 64) * 16);
+    }
+  }
+  __device__ inline void operator()(uint8_t* tile, const T* base, int64_t stride, uint64_t there, bool near) const {
+    if (near && there == (ROWS == 64 ? ~0ull : (1ull << ROWS) - 1)) whole(tile, base);
+    else some(tile, base, stride, there);
+  }
+};
 
 // Which of the KT keys from `first` on are valid, as bits.
 struct Keys {
   int n;                 // valid length
   const uint8_t* mask;   // the batch entry's, or NULL
-  __device__ inline Keys(const CrossArgs& a, int b) : n(a.kv_len ? max(0, min(a.kv_len[b], a.S)) : a.S), mask(a.kv_mask ? a.kv_mask + (int64_t)b * a.S : nullptr) {}
+  __device__ inline Keys(Args& a, int b) : n(a.kv_len ? max(0, min(a.kv_len[b], a.S)) : a.S), mask(a.kv_mask ? a.kv_mask + (int64_t)b * a.S : nullptr) {}
   __device__ inline uint64_t bits(int first, int count, int lane) const {
+    if (!mask) {  // (uniform: a length alone)
+      const int left = n - first;
+      return left >= count ? (count == 64 ? ~0ull : (1ull << count) - 1) : left <= 0 ? 0 : (1ull << left) - 1;
+    }
     const int s = first + lane;
-    bool ok = lane < count && s < n;
-    if (mask && ok) ok = mask[s] != 0;
-    return __ballot(ok);
+    const bool in = lane < count && s < n;
+    const uint8_t m = mask[in ? s : 0];
+    return __ballot(in && m != 0);
   }
 };
 
@@ -137,16 +186,30 @@ __device__ inline constexpr int d_row(int r) { return 8 * (r / 4) + (r % 4); }
 __device__ inline void store4(uint16_t* p, f32x4 v) { *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
 __device__ inline void store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
 
-// The column of a [DT x 32 channels][32 columns] accumulator as a row of d channels at p.
+// The column of a [DT x 32 channels][32 columns] accumulator as a row of d channels at p.  A lane has four channels of every
+// eight and its partner (lane ^ 32) the other four; for bf16 the two exchange them, so that each stores 16 bytes.
 template <typename T, int DT>
-__device__ inline void store_column(T* p, const f32x16 (&acc)[DT], float scale, int d, int grp) {
+__device__ inline void store_column(T* p, const f32x16 (&acc)[DT], float scale, int d, int grp, bool live) {
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+  for (int dt = 0; dt < DT; ++dt) {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      const int ch = 32 * dt + 8 * r4 + 4 * grp;
-      if (ch < d) store4(p + ch, f32x4{acc[dt][4 * r4], acc[dt][4 * r4 + 1], acc[dt][4 * r4 + 2], acc[dt][4 * r4 + 3]} * scale);
+      for (int k = 0; k < 2; ++k) {  // channels 16 k .. + 15 of the tile: this lane 8 grp .. + 7
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(acc[dt][8 * k + 2 * i] * scale, acc[dt][8 * k + 2 * i + 1] * scale);
+        const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        const int ch = 32 * dt + 16 * k + 8 * grp;
+        if (live && ch < d) *reinterpret_cast<u32x4*>(p + ch) = u32x4{x[0], y[0], x[1], y[1]};
+      }
+    } else {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int ch = 32 * dt + 8 * r4 + 4 * grp;
+        if (live && ch < d) store4(p + ch, f32x4{acc[dt][4 * r4], acc[dt][4 * r4 + 1], acc[dt][4 * r4 + 2], acc[dt][4 * r4 + 3]} * scale);
+      }
     }
+  }
 }
 
 template <typename T, int DT>

@@ -3,8 +3,7 @@
 //
 // The G query heads that share keys are one matrix of M = G Lq rows, so shared heads cost nothing in the forward and dQ and
 // their gradients come out summed.  A workgroup has four wavefronts of 32 rows (forward, dQ) or 32 keys (dK, dV); the other
-// side's tiles stream through LDS in a ring of two, one barrier a tile.  Where there are few workgroups, the walk is split into
-// segments whose fp32 partial results a second launch joins, in a fixed order.
+// side's tiles stream through LDS in a ring of two, one barrier a tile.
 #include <algorithm>
 
 #include "bsa_cross.h"
@@ -14,58 +13,148 @@ namespace bsa {
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kUnitRows = 32 * kWaves;
 
-template <typename T> constexpr int key_tile() { return sizeof(T) == 2 ? 64 : 32; }
+template <typename T, int DP> constexpr int key_tile() { return sizeof(T) == 2 && DP <= 128 ? 64 : 32; }
 
-// A launch's work: `units` of kUnitRows rows (keys) each, walked in `nseg` segments of `per` tiles.
-struct Plan {
-  int tiles, nseg, per;
-  int64_t units;
+// ---- how a launch's work is dealt out ----
+// A unit (kUnitRows query rows of one key head; dK and dV: a tile of keys) takes a number of steps (key tiles; query tiles).  Either
+// every unit is a workgroup's, or all steps of a launch, unit after unit, are cut into equal shares: a workgroup's first and
+// last piece may then be parts of a unit, whose fp32 results it leaves for a second launch that adds them up in
+// order.  Shares keep the chip full where units are few, long or (valid lengths) unlike.
+struct Deal {
+  int grid;      // workgroups
+  int shares;    // 0: workgroup n takes unit n
+  int by_keys;   // units are tiles of `tile` keys and take `steps` steps; else `rows` units an entry of a step per `tile` valid keys
+  int tile, steps;
+  int64_t rows;  // units of a batch entry: (by_keys) of S keys
 };
 
-// Segments only where the units leave half of the chip's 512 workgroup slots empty, and of four tiles at least.
-static Plan make_plan(int64_t units, int64_t tiles) {
-  Plan p;
-  p.units = units;
-  p.tiles = (int)tiles;
-  int64_t n = units * 2 > 512 ? 1 : std::min<int64_t>(512 / units, (tiles + 3) / 4);
-  if (n < 1) n = 1;
-  p.per = (int)((tiles + n - 1) / n);
-  p.nseg = (int)((tiles + p.per - 1) / p.per);
-  return p;
-}
-static int row_units(const CrossArgs& a) { return (a.M + kUnitRows - 1) / kUnitRows; }
-static Plan rows_plan(const CrossArgs& a) {
-  const int kt = a.dtype == BSA_F32 ? 32 : 64;
-  return make_plan((int64_t)a.B * a.Hkv * row_units(a), (a.S + kt - 1) / kt);
-}
-static int query_tiles(const CrossArgs& a) { return (a.Lq + 31) / 32; }  // of a head
-static Plan keys_plan(const CrossArgs& a) {
-  return make_plan((int64_t)a.B * a.Hkv * ((a.S + kUnitRows - 1) / kUnitRows), (int64_t)a.G * query_tiles(a));
-}
-static int padded_d(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+struct Ledger {
+  const Deal& dl;
+  const int* len;
+  int B, S, Hkv, lane;
+  __device__ inline Ledger(Args& a, const Deal& dl_, int lane_) : dl(dl_), len(a.kv_len), B(a.B), S(a.S), Hkv(a.Hkv), lane(lane_) {}
+  __device__ inline int valid(int b) const { return len ? max(0, min(len[b], S)) : S; }
+  __device__ inline int tiles(int b) const { return (valid(b) + dl.tile - 1) / dl.tile; }
+  __device__ inline int steps(int b) const { return dl.by_keys ? dl.steps : tiles(b); }
+  __device__ inline int64_t units(int b) const { return dl.by_keys ? (int64_t)Hkv * tiles(b) : dl.rows; }  // that take steps
+  __device__ inline int64_t weight(int b) const { return units(b) * steps(b); }
+  __device__ inline int64_t scan(int64_t v) const {  // inclusive, over the lanes
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t w = __shfl_up(v, o);
+      if (lane >= o) v += w;
+    }
+    return v;
+  }
+  // Steps of the entries below b (of all with b = B).
+  __device__ inline int64_t below(int b) const {
+    if (!len) return b * weight(0);
+    int64_t sum = 0;
+    for (int b0 = 0; b0 < b; b0 += 64) sum += __shfl(scan(b0 + lane < b ? weight(b0 + lane) : 0), 63);
+    return sum;
+  }
+  // The entry that step `pos` is of, and the step that it begins with.
+  __device__ inline int entry(int64_t pos, int64_t& base) const {
+    if (!len) {
+      const int64_t w = weight(0);
+      const int b = (int)(pos / w);
+      base = b * w;
+      return b;
+    }
+    base = 0;
+    for (int b0 = 0;; b0 += 64) {
+      const int64_t v = b0 + lane < B ? weight(b0 + lane) : 0, to = scan(v);
+      const uint64_t past = __ballot(base + to > pos);
+      if (past || b0 + 64 >= B) {
+        const int l = __builtin_amdgcn_readfirstlane(__builtin_ctzll(past | (1ull << 63)));
+        base += __shfl(to - v, l);
+        return b0 + l;
+      }
+      base += __shfl(to, 63);
+    }
+  }
+};
 
-// Partial results: [segment][unit][wavefront][value][lane] floats.
+// One piece of a workgroup's work: steps t0 .. t1 - 1 of a unit.
+struct Piece {
+  int b, t0, t1;
+  int64_t unit;   // of the entry
+  int slot;       // of its partial results; -1: the unit is whole
+};
+
+template <typename F>
+__device__ inline void for_pieces(Args& a, const Deal& dl, int lane, F work) {
+  const Ledger led(a, dl, lane);
+  int64_t pos = 0, begin = 0, end = 1, per = 1;
+  if (dl.shares) {
+    const int64_t total = led.below(a.B);
+    per = (total + dl.grid - 1) / dl.grid;
+    begin = pos = blockIdx.x * per;
+    end = min(begin + per, total);
+  }
+  while (pos < end) {
+    Piece pc;
+    if (dl.shares) {
+      int64_t base;
+      pc.b = led.entry(pos, base);
+      const int steps = led.steps(pc.b);
+      pc.unit = (pos - base) / steps;
+      pc.t0 = (int)(pos - base - pc.unit * steps);
+      pc.t1 = (int)min((int64_t)steps, pc.t0 + (end - pos));
+      pc.slot = pc.t0 == 0 && pc.t1 == steps ? -1 : 2 * (int)blockIdx.x + (pos != begin);
+      pos += pc.t1 - pc.t0;
+    } else {
+      pc.b = (int)(blockIdx.x / dl.rows);
+      pc.unit = blockIdx.x - pc.b * dl.rows;
+      pc.t0 = 0;
+      pc.t1 = led.steps(pc.b);
+      pc.slot = -1;
+      pos = end;
+    }
+    work(pc);
+  }
+}
+
+// The partial results of a unit of entry b: how many there are (0: the unit is whole, -1: nobody worked on it) and their slots.
+struct Parts {
+  int n;
+  int64_t per, first, w0;
+  __device__ inline Parts(Args& a, const Deal& dl, int lane, int b, int64_t unit) : n(-1), per(0), first(0), w0(0) {
+    const Ledger led(a, dl, lane);
+    const int steps = led.steps(b);
+    if (steps == 0 || unit >= led.units(b)) return;
+    const int64_t total = led.below(a.B);
+    per = (total + dl.grid - 1) / dl.grid;
+    first = led.below(b) + unit * steps;
+    w0 = first / per;
+    n = (int)((first + steps - 1) / per - w0);
+    if (n) ++n;
+  }
+  __device__ inline int64_t slot(int k) const { return 2 * (w0 + k) + ((w0 + k) * per < first); }
+};
+
+// Partial results: [slot][wavefront][value][lane] floats.
 template <int VALUES>
-__device__ inline float* part_of(float* base, int64_t units, int seg, int64_t unit, int wave, int lane) {
-  return base + (((seg * units + unit) * kWaves + wave) * VALUES) * 64 + lane;
+__device__ inline float* part_of(float* base, int64_t slot, int wave, int lane) {
+  return base + ((slot * kWaves + wave) * VALUES) * 64 + lane;
 }
 
 struct RowUnit {
-  int64_t unit;
   int b, hk, m, g, l;  // batch entry, key head, row, its head in the group and token
-  bool live;
-  __device__ inline RowUnit(const CrossArgs& a, int64_t unit_, int wave, int lane, int units_of_head) : unit(unit_) {
-    const int bh = (int)(unit / units_of_head);
-    b = bh / a.Hkv;
-    hk = bh - b * a.Hkv;
-    m = (int)(unit - (int64_t)bh * units_of_head) * kUnitRows + 32 * wave + (lane & 31);
+  bool live, any;      // this row, any of the wavefront's exists
+  __device__ inline RowUnit(Args& a, int b_, int64_t unit /* of the entry */, int wave, int lane) : b(b_) {
+    const int of_head = (a.M + kUnitRows - 1) / kUnitRows;
+    hk = (int)(unit / of_head);
+    const int first = (int)(unit - (int64_t)hk * of_head) * kUnitRows + 32 * wave;
+    any = first < a.M;
+    m = first + (lane & 31);
     live = m < a.M;
     g = live ? m / a.Lq : 0;
     l = live ? m - g * a.Lq : 0;
   }
-  __device__ inline int head(const CrossArgs& a) const { return hk * a.G + g; }
-  __device__ inline int64_t offset(const CrossArgs& a, const bsa_strides_t& s) const { return b * s.b + (int64_t)head(a) * s.h + (int64_t)l * s.l; }
-  __device__ inline int64_t flat(const CrossArgs& a) const { return ((int64_t)b * a.H + head(a)) * a.Lq + l; }
+  __device__ inline int head(Args& a) const { return hk * a.G + g; }
+  __device__ inline int64_t offset(Args& a, const __attribute__((address_space(4))) bsa_strides_t& s) const { return b * s.b + (int64_t)head(a) * s.h + (int64_t)l * s.l; }
+  __device__ inline int64_t flat(Args& a) const { return ((int64_t)b * a.H + head(a)) * a.Lq + l; }
 };
 
 // Chunk c of a row, zeros where there is none.
@@ -117,284 +206,322 @@ struct RowFrags {
     return sum;
   }
 };
+template <typename T, int DP> constexpr int two_a_cu() { return sizeof(T) == 2 && DP <= 128 ? 2 : 1; }
 template <typename T, int DP> constexpr bool held() { return DP * sizeof(T) <= 512; }  // one row beside an accumulator of DP channels
 
 // ---- forward ----
 // O = 0 and LSE = -inf without a valid key; a row whose valid logits are all -inf has no softmax and is NaN.
+__device__ inline void put_lse(Args& a, const RowUnit& u, float m, float l, bool any, int grp) {
+  if (grp == 0 && u.live) a.LSE_out[u.flat(a)] = any ? __builtin_fmaf(m, a.sm_scale, __builtin_amdgcn_logf(l) * kLn2) : -INFINITY;
+}
 template <typename T, int DT>
-__device__ inline void finish_row(const CrossArgs& a, const RowUnit& u, const f32x16 (&acc)[DT], float m, float l, bool any, int grp) {
-  if (!u.live) return;
-  store_column<T, DT>(static_cast<T*>(a.O_out) + u.offset(a, a.o), acc, any ? 1.f / l : 0.f, a.d, grp);
-  if (grp == 0) a.LSE_out[u.flat(a)] = any ? __builtin_fmaf(m, a.sm_scale, __builtin_amdgcn_logf(l) * kLn2) : -INFINITY;
+__device__ inline void finish_row(Args& a, const RowUnit& u, const f32x16 (&acc)[DT], float m, float l, bool any, int grp) {
+  store_column<T, DT>(static_cast<T*>(a.O_out) + u.offset(a, a.o), acc, any ? 1.f / l : 0.f, a.d, grp, u.live);
+  put_lse(a, u, m, l, any, grp);
 }
 
+// The K and V tiles of a piece on their way through the ring of two.
 template <typename T, int DP>
-__global__ __launch_bounds__(kThreads, 1) void cross_fwd_kernel(CrossArgs a, Plan plan, int units_of_head, float* part) {
+struct KvRing {
+  static constexpr int KT = key_tile<T, DP>(), TILE = KT * DP * (int)sizeof(T);
+  uint8_t* smem;
+  Requests<T, DP, KT, kThreads> rk, rv;
+  int lane;
+  __device__ inline KvRing(uint8_t* smem_, Args& a, int tid) : smem(smem_), rk(a.k.l, a.d, tid), rv(a.v.l, a.d, tid), lane(tid & 63) {
+    if (a.d < DP)
+      for (int k = 0; k < 4; ++k) rk.clear(smem + k * TILE);
+  }
+  __device__ inline const uint8_t* k_tile(int t) const { return smem + (t & 1) * 2 * TILE; }
+  __device__ inline const uint8_t* v_tile(int t) const { return k_tile(t) + TILE; }
+  // returns the valid keys of tile t
+  __device__ inline uint64_t request(Args& a, int b, int hk, const Keys& keys, int t) const {
+    const uint64_t there = keys.bits(t * KT, KT, lane);
+    const T* K = static_cast<const T*>(a.K) + b * a.k.b + hk * a.k.h + (int64_t)t * KT * a.k.l;
+    const T* V = static_cast<const T*>(a.V) + b * a.v.b + hk * a.v.h + (int64_t)t * KT * a.v.l;
+    uint8_t* at = smem + (t & 1) * 2 * TILE;
+    rk(at, K, a.k.l, there, a.near);
+    rv(at + TILE, V, a.v.l, there, a.near);
+    return there;
+  }
+  static constexpr uint64_t ALL = KT == 64 ? ~0ull : (1ull << KT) - 1;
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_fwd_kernel(CrossArgs, Deal dl, float* part) {
   using E = Elt<T>;
-  constexpr int KT = key_tile<T>(), NK = KT / 32, DT = DP / 32, TILE = KT * DP * sizeof(T);
+  using Ring = KvRing<T, DP>;
+  constexpr int KT = key_tile<T, DP>(), NK = KT / 32, DT = DP / 32;
   extern __shared__ __align__(16) uint8_t smem[];  // [2][K tile | V tile]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 5;
-  const int seg = (int)(blockIdx.x / plan.units);
-  const RowUnit u(a, blockIdx.x % plan.units, wave, lane, units_of_head);
-  const Keys keys(a, u.b);
   const TileView<T, DP> view(lane);
-  const T* K = static_cast<const T*>(a.K) + u.b * a.k.b + u.hk * a.k.h;
-  const T* V = static_cast<const T*>(a.V) + u.b * a.v.b + u.hk * a.v.h;
+  const Ring ring(smem, *kernel_args(), tid);
 
-  const RowFrags<T, DP, held<T, DP>()> q(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
-  f32x16 o[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-  float m = -INFINITY, l = 0.f;
-  const float c = a.sm_scale * kLog2e;
-  bool any = false;
-  const int t0 = seg * plan.per, t1 = min(t0 + plan.per, (keys.n + KT - 1) / KT);
-  uint64_t bits = 0;
-  auto request = [&](int t) -> uint64_t {
-    const uint64_t there = keys.bits(t * KT, KT, lane);
-    uint8_t* at = smem + (t & 1) * 2 * TILE;
-    request_tile<T, DP, KT, kThreads>(at, K + (int64_t)t * KT * a.k.l, a.k.l, there, a.d, tid);
-    request_tile<T, DP, KT, kThreads>(at + TILE, V + (int64_t)t * KT * a.v.l, a.v.l, there, a.d, tid);
-    return there;
-  };
-  if (t0 < t1) bits = request(t0);
-  for (int t = t0; t < t1; ++t) {
-    wait_vm<0>();
-    raw_barrier();
-    const uint64_t now = bits;
-    if (t + 1 < t1) bits = request(t + 1);
-    if (now == 0) continue;
-    any = true;
-    const uint8_t* kt = smem + (t & 1) * 2 * TILE;
-    const uint8_t* vt = kt + TILE;
-    f32x16 s[NK];
-#pragma unroll
-    for (int k = 0; k < NK; ++k)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[k][r] = 0.f;
-#pragma unroll
-    for (int k = 0; k < NK; ++k) q.times(s[k], view, kt, 32 * k);
-    if (now != (KT == 64 ? ~0ull : 0xffffffffull)) {
-      const uint64_t own = now >> (4 * grp);
-#pragma unroll
-      for (int k = 0; k < NK; ++k)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!((own >> (32 * k + d_row(r))) & 1)) s[k][r] = -INFINITY;
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int k = 0; k < NK; ++k)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
-    top = pair_max(top);
-    if (__any(top > m)) {
-      const float next = fmaxf(m, top);
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - next) * c);
-      m = next;
-      l *= f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[dt][r] *= f;
-    }
-    const float base = m == -INFINITY ? 0.f : m * c;  // (all logits so far are -inf: they weigh nothing)
-#pragma unroll
-    for (int k = 0; k < NK; ++k)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], c, -base));
-        l += s[k][r];
-      }
-#pragma unroll
-    for (int k = 0; k < NK; ++k)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const auto p = E::column(s[k], h);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) E::mma8(o[dt], view.along(vt, 32 * k + 16 * h, dt), p);
-      }
-  }
-  l = pair_sum(l);
-  if (plan.nseg == 1) {
-    finish_row<T, DT>(a, u, o, m, l, any, grp);
-    return;
-  }
-  float* out = part_of<DT * 16 + 2>(part, plan.units, seg, u.unit, wave, lane);
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = o[dt][r];
-  out[DT * 16 * 64] = m;
-  out[(DT * 16 + 1) * 64] = any ? l : -1.f;  // (a sum is never negative)
-}
-
-template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void cross_fwd_combine_kernel(CrossArgs a, Plan plan, int units_of_head, float* part) {
-  constexpr int DT = DP / 32, VALUES = DT * 16 + 2;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const RowUnit u(a, blockIdx.x, wave, lane, units_of_head);
-  const float c = a.sm_scale * kLog2e;
-  float m = -INFINITY;
-  bool any = false;
-  for (int s = 0; s < plan.nseg; ++s) {
-    const float* in = part_of<VALUES>(part, plan.units, s, u.unit, wave, lane);
-    if (in[(DT * 16 + 1) * 64] == -1.f) continue;
-    any = true;
-    m = fmaxf(m, in[DT * 16 * 64]);
-  }
-  f32x16 o[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-  float l = 0.f;
-  for (int s = 0; s < plan.nseg; ++s) {
-    const float* in = part_of<VALUES>(part, plan.units, s, u.unit, wave, lane);
-    const float ls = in[(DT * 16 + 1) * 64], ms = in[DT * 16 * 64];
-    if (ls == -1.f) continue;
-    const float f = ms == -INFINITY && ls == 0.f ? 0.f : __builtin_amdgcn_exp2f((ms - m) * c);
-    l = __builtin_fmaf(ls, f, l);
+  for_pieces(*kernel_args(), dl, lane, [&](const Piece& pc) {
+    Args& a = *afresh(kernel_args());
+    const float c = a.sm_scale * kLog2e;
+    const RowUnit u(a, pc.b, pc.unit, wave, lane);
+    const Keys keys(a, u.b);
+    raw_barrier();  // the ring is free
+    uint64_t bits = pc.t0 < pc.t1 ? ring.request(a, u.b, u.hk, keys, pc.t0) : 0;
+    const RowFrags<T, DP, held<T, DP>()> q(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
+    f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[dt][r] = __builtin_fmaf(in[(dt * 16 + r) * 64], f, o[dt][r]);
+      for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    bool any = false;
+    for (int t = pc.t0; t < pc.t1; ++t) {
+      wait_vm<0>();
+      raw_barrier();
+      const uint64_t now = bits;
+      if (t + 1 < pc.t1) bits = ring.request(a, u.b, u.hk, keys, t + 1);
+      if (now == 0 || !u.any) continue;
+      any = true;
+      const uint8_t* kt = ring.k_tile(t);
+      const uint8_t* vt = ring.v_tile(t);
+      f32x16 s[NK];
+#pragma unroll
+      for (int k = 0; k < NK; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[k][r] = 0.f;
+#pragma unroll
+      for (int k = 0; k < NK; ++k) q.times(s[k], view, kt, 32 * k);
+      if (now != Ring::ALL) {
+        const uint64_t own = now >> (4 * grp);
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!((own >> (32 * k + d_row(r))) & 1)) s[k][r] = -INFINITY;
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int k = 0; k < NK; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
+      top = pair_max(top);
+      if (__any(top > m)) {
+        const float next = fmaxf(m, top);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - next) * c);
+        m = next;
+        l *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+      }
+      const float base = m == -INFINITY ? 0.f : m * c;  // (all logits so far are -inf: they weigh nothing)
+#pragma unroll
+      for (int k = 0; k < NK; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], c, -base));
+          l += s[k][r];
+        }
+#pragma unroll
+      for (int k = 0; k < NK; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const auto p = E::column(s[k], h);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) E::mma8(o[dt], view.along(vt, 32 * k + 16 * h, dt), p);
+        }
+    }
+    if (!u.any) return;
+    l = pair_sum(l);
+    if (pc.slot < 0) {
+      finish_row<T, DT>(a, u, o, m, l, any, grp);
+      return;
+    }
+    float* out = part_of<DT * 16 + 2>(part, pc.slot, wave, lane);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = o[dt][r];
+    out[DT * 16 * 64] = m;
+    out[(DT * 16 + 1) * 64] = any ? l : -1.f;  // (a sum is never negative)
+  });
+}
+
+// Sum over the parts of a unit of the 16 values that a wavefront's channel tile has at `at` (values before it), each part times its
+// weight: four parts' loads in flight.
+template <int VALUES, typename F>
+__device__ inline f32x16 sum_parts(float* part, const Parts& ps, int at, int wave, int lane, F weight) {
+  f32x16 acc;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+  for (int s = 0; s < ps.n; s += 4) {
+    float v[4][16], f[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float* in = part_of<VALUES>(part, ps.slot(min(s + j, ps.n - 1)), wave, lane) + at * 64;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v[j][r] = in[r * 64];
+      f[j] = weight(min(s + j, ps.n - 1));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (s + j < ps.n && f[j] != 0.f)  // (a part without a valid key holds nothing)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = __builtin_fmaf(v[j][r], f[j], acc[r]);
   }
-  finish_row<T, DT>(a, u, o, m, l, any, lane >> 5);
+  return acc;
+}
+
+// Joins the parts of a unit, and writes the rows of the units that had no step.  A workgroup has a wavefront for every 32 channels
+// of the rows of one of the walk's wavefronts (blockIdx.y).
+template <typename T, int DP>
+__global__ __launch_bounds__(2 * DP, 1) void cross_fwd_combine_kernel(CrossArgs, Deal dl, float* part) {
+  Args& a = *kernel_args();
+  constexpr int DT = DP / 32, VALUES = DT * 16 + 2;
+  const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.y, grp = lane >> 5;
+  const int b = (int)(blockIdx.x / dl.rows);
+  const int64_t unit = blockIdx.x - b * dl.rows;
+  const RowUnit u(a, b, unit, wave, lane);
+  if (!u.any) return;
+  const Parts ps(a, dl, lane, b, unit);
+  if (ps.n == 0) return;
+  const float c = a.sm_scale * kLog2e;
+  auto top_of = [&](int s) { return part_of<VALUES>(part, ps.slot(s), wave, lane)[DT * 16 * 64]; };
+  auto sum_of = [&](int s) { return part_of<VALUES>(part, ps.slot(s), wave, lane)[(DT * 16 + 1) * 64]; };
+  float m = -INFINITY, l = 0.f;
+  bool any = false;
+#pragma unroll 4
+  for (int s = 0; s < ps.n; ++s) {
+    const float ms = top_of(s), ls = sum_of(s);
+    any |= ls != -1.f;
+    m = fmaxf(m, ls == -1.f ? -INFINITY : ms);
+  }
+  auto weight = [&](int s) {
+    const float ms = top_of(s), ls = sum_of(s);
+    return ls == -1.f || (ms == -INFINITY && ls == 0.f) ? 0.f : __builtin_amdgcn_exp2f((ms - m) * c);
+  };
+#pragma unroll 4
+  for (int s = 0; s < ps.n; ++s) {
+    const float ls = sum_of(s);
+    l = __builtin_fmaf(ls == -1.f ? 0.f : ls, weight(s), l);
+  }
+  const f32x16 o[1] = {sum_parts<VALUES>(part, ps, dt * 16, wave, lane, weight)};
+  store_column<T, 1>(static_cast<T*>(a.O_out) + u.offset(a, a.o) + 32 * dt, o, any ? 1.f / l : 0.f, a.d - 32 * dt, grp, u.live);
+  if (dt == 0) put_lse(a, u, m, l, any, grp);
 }
 
 // ---- dQ ----
 // dQ^T += K^T dS^T over the key tiles, S^T and dP^T recomputed.  Ahead of the walk each wavefront forms delta of its rows and leaves
 // (LSE, -delta) for the other kernel: per head and 32 tokens [32] LSE log2(e), [32] -delta; tokens past the last
 // have LSE = +inf, i.e. weights of zero.
-template <typename T, int DP>
-__global__ __launch_bounds__(kThreads, 1) void cross_dq_kernel(CrossArgs a, Plan plan, int units_of_head, float* stat, float* part) {
-  using E = Elt<T>;
-  constexpr int KT = key_tile<T>(), NK = KT / 32, DT = DP / 32, TILE = KT * DP * sizeof(T);
-  extern __shared__ __align__(16) uint8_t smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 5;
-  const int seg = (int)(blockIdx.x / plan.units);
-  const RowUnit u(a, blockIdx.x % plan.units, wave, lane, units_of_head);
-  const Keys keys(a, u.b);
-  const TileView<T, DP> view(lane);
-  const T* K = static_cast<const T*>(a.K) + u.b * a.k.b + u.hk * a.k.h;
-  const T* V = static_cast<const T*>(a.V) + u.b * a.v.b + u.hk * a.v.h;
-
-  const RowFrags<T, DP, held<T, DP>()> q(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
-  const RowFrags<T, DP, DP <= 128> gr(static_cast<const T*>(a.dO) + u.offset(a, a.go), u.live, a.d, grp);
-  float delta = gr.dot(static_cast<const T*>(a.O) + u.offset(a, a.o));
-  delta = pair_sum(delta);
-  const float lse2 = u.live ? a.LSE_in[u.flat(a)] * kLog2e : INFINITY;
-  if (seg == 0 && grp == 0 && u.live) {
-    const int tiles = (a.Lq + 31) / 32;
-    float* at = stat + (((int64_t)u.b * a.H + u.head(a)) * tiles + (u.l >> 5)) * 64;
-    at[u.l & 31] = lse2;
-    at[32 + (u.l & 31)] = -delta;
-    if (u.l == a.Lq - 1)
-      for (int i = (u.l & 31) + 1; i < 32; ++i) {
-        at[i] = INFINITY;
-        at[32 + i] = 0.f;
-      }
-  }
-
-  f32x16 dq[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dq[dt][r] = 0.f;
-  const float c = a.sm_scale * kLog2e;
-  const int t0 = seg * plan.per, t1 = min(t0 + plan.per, (keys.n + KT - 1) / KT);
-  uint64_t bits = 0;
-  auto request = [&](int t) -> uint64_t {
-    const uint64_t there = keys.bits(t * KT, KT, lane);
-    uint8_t* at = smem + (t & 1) * 2 * TILE;
-    request_tile<T, DP, KT, kThreads>(at, K + (int64_t)t * KT * a.k.l, a.k.l, there, a.d, tid);
-    request_tile<T, DP, KT, kThreads>(at + TILE, V + (int64_t)t * KT * a.v.l, a.v.l, there, a.d, tid);
-    return there;
-  };
-  if (t0 < t1) bits = request(t0);
-  for (int t = t0; t < t1; ++t) {
-    wait_vm<0>();
-    raw_barrier();
-    const uint64_t now = bits;
-    if (t + 1 < t1) bits = request(t + 1);
-    if (now == 0) continue;
-    const uint8_t* kt = smem + (t & 1) * 2 * TILE;
-    const uint8_t* vt = kt + TILE;
-    const uint64_t own = now >> (4 * grp);
-    const bool whole = now == (KT == 64 ? ~0ull : 0xffffffffull);
-#pragma unroll
-    for (int k = 0; k < NK; ++k) {
-      f32x16 s, dp;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
-      q.times(s, view, kt, 32 * k);
-      gr.times(dp, view, vt, 32 * k);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
-      if (!whole)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!((own >> (32 * k + d_row(r))) & 1)) s[r] = 0.f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const auto ds = E::column(s, h);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) E::mma8(dq[dt], view.along(kt, 32 * k + 16 * h, dt), ds);
-      }
+__device__ inline void put_stat(Args& a, const RowUnit& u, float* stat, float lse2, float delta, int grp) {
+  if (grp != 0 || !u.live) return;
+  const int tiles = (a.Lq + 31) / 32;
+  float* at = stat + (((int64_t)u.b * a.H + u.head(a)) * tiles + (u.l >> 5)) * 64;
+  at[u.l & 31] = lse2;
+  at[32 + (u.l & 31)] = -delta;
+  if (u.l == a.Lq - 1)
+    for (int i = (u.l & 31) + 1; i < 32; ++i) {
+      at[i] = INFINITY;
+      at[32 + i] = 0.f;
     }
-  }
-  if (plan.nseg == 1) {
-    if (u.live) store_column<T, DT>(static_cast<T*>(a.dQ) + u.offset(a, a.gq), dq, a.sm_scale, a.d, grp);
-    return;
-  }
-  float* out = part_of<DT * 16>(part, plan.units, seg, u.unit, wave, lane);
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = dq[dt][r];
 }
 
-template <int DT>
-__device__ inline void sum_parts(f32x16 (&acc)[DT], float* part, const Plan& plan, int64_t unit, int wave, int lane) {
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[dt][r] = 0.f;
-  for (int s = 0; s < plan.nseg; ++s) {
-    const float* in = part_of<DT * 16>(part, plan.units, s, unit, wave, lane);
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel(CrossArgs, Deal dl, float* stat, float* part) {
+  using E = Elt<T>;
+  using Ring = KvRing<T, DP>;
+  constexpr int KT = key_tile<T, DP>(), NK = KT / 32, DT = DP / 32;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 5;
+  const TileView<T, DP> view(lane);
+  const Ring ring(smem, *kernel_args(), tid);
+
+  for_pieces(*kernel_args(), dl, lane, [&](const Piece& pc) {
+    Args& a = *afresh(kernel_args());
+    const float c = a.sm_scale * kLog2e;
+    const RowUnit u(a, pc.b, pc.unit, wave, lane);
+    const Keys keys(a, u.b);
+    raw_barrier();
+    uint64_t bits = pc.t0 < pc.t1 ? ring.request(a, u.b, u.hk, keys, pc.t0) : 0;
+    const RowFrags<T, DP, held<T, DP>()> q(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
+    const RowFrags<T, DP, DP <= 128> gr(static_cast<const T*>(a.dO) + u.offset(a, a.go), u.live, a.d, grp);
+    const float delta = pair_sum(gr.dot(static_cast<const T*>(a.O) + u.offset(a, a.o)));
+    const float lse2 = u.live ? a.LSE_in[u.flat(a)] * kLog2e : INFINITY;
+    if (pc.t0 == 0) put_stat(a, u, stat, lse2, delta, grp);
+    f32x16 dq[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[dt][r] += in[(dt * 16 + r) * 64];
-  }
+      for (int r = 0; r < 16; ++r) dq[dt][r] = 0.f;
+    for (int t = pc.t0; t < pc.t1; ++t) {
+      wait_vm<0>();
+      raw_barrier();
+      const uint64_t now = bits;
+      if (t + 1 < pc.t1) bits = ring.request(a, u.b, u.hk, keys, t + 1);
+      if (now == 0 || !u.any) continue;
+      const uint8_t* kt = ring.k_tile(t);
+      const uint8_t* vt = ring.v_tile(t);
+      const uint64_t own = now >> (4 * grp);
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        __builtin_amdgcn_sched_barrier(0);  // one half at a time in the registers
+        f32x16 s, dp;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+        q.times(s, view, kt, 32 * k);
+        gr.times(dp, view, vt, 32 * k);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
+        if (now != Ring::ALL)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!((own >> (32 * k + d_row(r))) & 1)) s[r] = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const auto ds = E::column(s, h);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) E::mma8(dq[dt], view.along(kt, 32 * k + 16 * h, dt), ds);
+        }
+      }
+    }
+    if (!u.any) return;
+    if (pc.slot < 0) {
+      store_column<T, DT>(static_cast<T*>(a.dQ) + u.offset(a, a.gq), dq, a.sm_scale, a.d, grp, u.live);
+      return;
+    }
+    float* out = part_of<DT * 16>(part, pc.slot, wave, lane);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = dq[dt][r];
+  });
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void cross_dq_combine_kernel(CrossArgs a, Plan plan, int units_of_head, float* part) {
+__global__ __launch_bounds__(2 * DP, 1) void cross_dq_combine_kernel(CrossArgs, Deal dl, float* part) {
+  Args& a = *kernel_args();
   constexpr int DT = DP / 32;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const RowUnit u(a, blockIdx.x, wave, lane, units_of_head);
-  f32x16 dq[DT];
-  sum_parts<DT>(dq, part, plan, u.unit, wave, lane);
-  if (u.live) store_column<T, DT>(static_cast<T*>(a.dQ) + u.offset(a, a.gq), dq, a.sm_scale, a.d, lane >> 5);
+  const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.y;
+  const int b = (int)(blockIdx.x / dl.rows);
+  const int64_t unit = blockIdx.x - b * dl.rows;
+  const RowUnit u(a, b, unit, wave, lane);
+  if (!u.any) return;
+  const Parts ps(a, dl, lane, b, unit);
+  if (ps.n == 0) return;
+  const f32x16 dq[1] = {sum_parts<DT * 16>(part, ps, dt * 16, wave, lane, [](int) { return 1.f; })};
+  store_column<T, 1>(static_cast<T*>(a.dQ) + u.offset(a, a.gq) + 32 * dt, dq, a.sm_scale, a.d - 32 * dt, lane >> 5, u.live);
 }
 
 // ---- dK, dV ----
 // A wavefront owns 32 keys; dV^T += dO^T P and dK^T += Q^T dS over the query tiles (32 tokens of one head) of the heads that share them.
+// (Units of an entry: key tile after key tile, each for all key heads, so that those with valid keys come first.)
 struct KeyUnit {
-  int64_t unit;
   int b, hk, first, key;
   bool there;   // the lane's key exists
-  __device__ inline KeyUnit(const CrossArgs& a, int64_t unit_, int wave, int lane, int units_of_head) : unit(unit_) {
-    const int bh = (int)(unit / units_of_head);
-    b = bh / a.Hkv;
-    hk = bh - b * a.Hkv;
-    first = (int)(unit - (int64_t)bh * units_of_head) * kUnitRows;
+  __device__ inline KeyUnit(Args& a, int b_, int64_t unit, int wave, int lane) : b(b_) {
+    const int tile = (int)(unit / a.Hkv);
+    hk = (int)(unit - (int64_t)tile * a.Hkv);
+    first = tile * kUnitRows;
     key = first + 32 * wave + (lane & 31);
     there = key < a.S;
   }
@@ -405,16 +532,24 @@ struct KeyUnit {
 enum { BOTH = 0, ONLY_K = 1, ONLY_V = 2 };
 
 template <typename T, int DP, int WHAT>
-__device__ inline void dkv_walk(CrossArgs a, Plan plan, int units_of_head, const float* stat, float* part) {
+__device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) {
   using E = Elt<T>;
   constexpr int DT = DP / 32, TILE = 32 * DP * sizeof(T), STAGE = 2 * TILE + 256;
   constexpr bool WITH_K = WHAT != ONLY_V, WITH_V = WHAT != ONLY_K;
   extern __shared__ __align__(16) uint8_t smem[];  // [2][Q tile | dO tile | LSE, -delta]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 5;
-  const int seg = (int)(blockIdx.x / plan.units);
-  const KeyUnit u(a, blockIdx.x % plan.units, wave, lane, units_of_head);
-  const Keys keys(a, u.b);
   const TileView<T, DP> view(lane);
+  Args& args = *kernel_args();
+  const Requests<T, DP, 32, kThreads> rq(args.q.l, args.d, tid), rg(args.go.l, args.d, tid);
+  if (args.d < DP)
+    for (int k = 0; k < 4; ++k) rq.clear(smem + (k >> 1) * STAGE + (k & 1) * TILE);
+ for_pieces(args, dl, lane, [&](const Piece& pc) {
+  Args& a = *afresh(kernel_args());
+  const float c = a.sm_scale * kLog2e;
+  const int tiles = (a.Lq + 31) / 32;  // of a head
+  const KeyUnit u(a, pc.b, pc.unit, wave, lane);
+  const Keys keys(a, u.b);
+  raw_barrier();
   const uint64_t mine = keys.bits(u.first + 32 * wave, 32, lane);                   // valid keys of the wavefront
   const bool valid = (mine >> (lane & 31)) & 1;
   const bool work = __syncthreads_or(mine != 0);                                   // of the workgroup
@@ -429,17 +564,15 @@ __device__ inline void dkv_walk(CrossArgs a, Plan plan, int units_of_head, const
       if (WITH_K) dk[dt][r] = 0.f;
       if (WITH_V) dv[dt][r] = 0.f;
     }
-  const float c = a.sm_scale * kLog2e;
-  const int tiles = (a.Lq + 31) / 32;  // of a head
-  const int t0 = seg * plan.per, t1 = work ? min(t0 + plan.per, plan.tiles) : t0;
+  const int t0 = pc.t0, t1 = work ? pc.t1 : t0;
   auto request = [&](int t) {
     const int g = t / tiles, i = t - g * tiles, head = u.hk * a.G + g, left = a.Lq - 32 * i;
     const uint64_t there = left >= 32 ? 0xffffffffull : (1ull << left) - 1;
     uint8_t* at = smem + (t & 1) * STAGE;
     const T* Q = static_cast<const T*>(a.Q) + u.b * a.q.b + (int64_t)head * a.q.h + (int64_t)32 * i * a.q.l;
     const T* G = static_cast<const T*>(a.dO) + u.b * a.go.b + (int64_t)head * a.go.h + (int64_t)32 * i * a.go.l;
-    request_tile<T, DP, 32, kThreads>(at, Q, a.q.l, there, a.d, tid);
-    request_tile<T, DP, 32, kThreads>(at + TILE, G, a.go.l, there, a.d, tid);
+    rq(at, Q, a.q.l, there, a.near);
+    rg(at + TILE, G, a.go.l, there, a.near);
     if (tid < 16) dma16(stat + (((int64_t)u.b * a.H + head) * tiles + i) * 64 + 4 * tid, at + 2 * TILE);
   };
   if (t0 < t1) request(t0);
@@ -481,96 +614,126 @@ __device__ inline void dkv_walk(CrossArgs a, Plan plan, int units_of_head, const
     }
   }
   // what a key that is not valid has gathered is no number of its own: its gradient is zero
-  auto put = [&](const f32x16 (&acc)[DT], void* to, const bsa_strides_t& st, float scale, int place) {
-    if (plan.nseg > 1) {
-      float* out = part_of<DT * 32>(part, plan.units, seg, u.unit, wave, lane) + place * DT * 16 * 64;
+  auto put = [&](const f32x16 (&acc)[DT], void* to, const __attribute__((address_space(4))) bsa_strides_t& st, float scale, int place) {
+    if (pc.slot >= 0) {
+      float* out = part_of<DT * 32>(part, pc.slot, wave, lane) + place * DT * 16 * 64;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = valid ? acc[dt][r] : 0.f;
-    } else if (u.there) {
+    } else {
       T* out = static_cast<T*>(to) + u.b * st.b + u.hk * st.h + u.key * st.l;
-      if (valid) store_column<T, DT>(out, acc, scale, a.d, grp);
-      else store_zeros<T, DT>(out, a.d, grp);
+      store_column<T, DT>(out, acc, scale, a.d, grp, valid);
+      if (u.there && !valid) store_zeros<T, DT>(out, a.d, grp);
     }
   };
   if constexpr (WITH_K) put(dk, a.dK, a.gk, a.sm_scale, 0);
   if constexpr (WITH_V) put(dv, a.dV, a.gv, 1.f, 1);
+ });
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(kThreads, 1) void cross_dkv_kernel(CrossArgs a, Plan plan, int units_of_head, const float* stat, float* part) {
-  if constexpr (DP <= 128) dkv_walk<T, DP, BOTH>(a, plan, units_of_head, stat, part);
-  else if (blockIdx.y == 0) dkv_walk<T, DP, ONLY_K>(a, plan, units_of_head, stat, part);
-  else dkv_walk<T, DP, ONLY_V>(a, plan, units_of_head, stat, part);
+__global__ __launch_bounds__(kThreads, 1) void cross_dkv_kernel(CrossArgs, Deal dl, const float* stat, float* part) {
+  if constexpr (DP <= 128) dkv_walk<T, DP, BOTH>(dl, stat, part);
+  else if (blockIdx.y == 0) dkv_walk<T, DP, ONLY_K>(dl, stat, part);
+  else dkv_walk<T, DP, ONLY_V>(dl, stat, part);
 }
 
+// Joins the parts of a unit, and writes the zeros of the units that had no step.
 template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void cross_dkv_combine_kernel(CrossArgs a, Plan plan, int units_of_head, float* part) {
+__global__ __launch_bounds__(2 * DP, 1) void cross_dkv_combine_kernel(CrossArgs, Deal dl, float* part) {
+  Args& a = *kernel_args();
   constexpr int DT = DP / 32;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, grp = lane >> 5;
-  const KeyUnit u(a, blockIdx.x, wave, lane, units_of_head);
-  const bool is_v = blockIdx.y;
-  f32x16 acc[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[dt][r] = 0.f;
-  for (int s = 0; s < plan.nseg; ++s) {
-    const float* in = part_of<DT * 32>(part, plan.units, s, u.unit, wave, lane) + (is_v ? DT * 16 * 64 : 0);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[dt][r] += in[(dt * 16 + r) * 64];
-  }
-  if (!u.there) return;
-  if (is_v) store_column<T, DT>(static_cast<T*>(a.dV) + u.b * a.gv.b + u.hk * a.gv.h + u.key * a.gv.l, acc, 1.f, a.d, grp);
-  else store_column<T, DT>(static_cast<T*>(a.dK) + u.b * a.gk.b + u.hk * a.gk.h + u.key * a.gk.l, acc, a.sm_scale, a.d, grp);
+  const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.y;
+  const bool is_v = blockIdx.z;
+  const int b = (int)(blockIdx.x / dl.rows);
+  const int64_t unit = blockIdx.x - b * dl.rows;
+  const KeyUnit u(a, b, unit, wave, lane);
+  const Parts ps(a, dl, lane, b, unit);
+  if (ps.n == 0) return;
+  const f32x16 acc[1] = {sum_parts<DT * 32>(part, ps, (is_v * DT + dt) * 16, wave, lane, [](int) { return 1.f; })};
+  const auto& st = is_v ? a.gv : a.gk;
+  store_column<T, 1>(static_cast<T*>(is_v ? a.dV : a.dK) + u.b * st.b + u.hk * st.h + u.key * st.l + 32 * dt, acc, is_v ? 1.f : a.sm_scale,
+                     a.d - 32 * dt, lane >> 5, u.there);
 }
 
 // ---- host ----
-static size_t part_bytes(const Plan& p, int values) { return p.nseg == 1 ? 0 : (size_t)p.nseg * p.units * kWaves * values * 64 * sizeof(float); }
+static int padded_d(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-size_t cross_fwd_workspace(const CrossArgs& a) { return part_bytes(rows_plan(a), padded_d(a.d) / 2 + 2); }
+// Forward and dQ.  Two workgroups a CU.
+static Deal rows_deal(const CrossArgs& a) {
+  Deal d{};
+  d.tile = a.dtype == BSA_BF16 && a.d <= 128 ? 64 : 32;  // key_tile
+  d.rows = (int64_t)a.Hkv * ((a.M + kUnitRows - 1) / kUnitRows);
+  const int64_t units = d.rows * a.B, tiles = (a.S + d.tile - 1) / d.tile;
+  d.shares = units < 2 * 512 && tiles > 4;
+  d.grid = (int)(d.shares ? std::max<int64_t>(units, std::min<int64_t>(512, units * tiles / 4)) : units);
+  return d;
+}
+
+static int query_tiles(const CrossArgs& a) { return (a.Lq + 31) / 32; }  // of a head
+
+static Deal keys_deal(const CrossArgs& a) {
+  Deal d{};
+  d.by_keys = 1;
+  d.tile = kUnitRows;
+  d.steps = a.G * query_tiles(a);
+  d.rows = (int64_t)a.Hkv * ((a.S + kUnitRows - 1) / kUnitRows);
+  const int64_t units = d.rows * a.B;
+  d.shares = 1;
+  d.grid = (int)std::min<int64_t>(256, std::max<int64_t>(units, units * d.steps / 4));
+  return d;
+}
+
+static size_t part_bytes(const Deal& d, int values) { return d.shares ? (size_t)2 * d.grid * kWaves * values * 64 * sizeof(float) : 0; }
+
+size_t cross_fwd_workspace(const CrossArgs& a) { return part_bytes(rows_deal(a), padded_d(a.d) / 2 + 2); }
 
 static size_t stat_bytes(const CrossArgs& a) { return (size_t)a.B * a.H * query_tiles(a) * 256; }
 
 size_t cross_bwd_workspace(const CrossArgs& a) {
-  return stat_bytes(a) + std::max(part_bytes(rows_plan(a), padded_d(a.d) / 2), part_bytes(keys_plan(a), padded_d(a.d)));
+  return stat_bytes(a) + std::max(part_bytes(rows_deal(a), padded_d(a.d) / 2), part_bytes(keys_deal(a), padded_d(a.d)));
 }
 
 template <typename T, int DP>
 static int fwd_t(const CrossArgs& a, hipStream_t st) {
-  const Plan p = rows_plan(a);
-  constexpr size_t lds = 4 * key_tile<T>() * DP * sizeof(T);
+  const Deal d = rows_deal(a);
+  constexpr size_t lds = 4 * key_tile<T, DP>() * DP * sizeof(T);
   if (const int rc = allow_dynamic_lds<cross_fwd_kernel<T, DP>>(lds)) return rc;
   float* part = static_cast<float*>(a.ws);
-  hipLaunchKernelGGL((cross_fwd_kernel<T, DP>), dim3((unsigned)(p.units * p.nseg)), dim3(kThreads), lds, st, a, p, row_units(a), part);
+  hipLaunchKernelGGL((cross_fwd_kernel<T, DP>), dim3(d.grid), dim3(kThreads), lds, st, a, d, part);
   if (const int rc = check_launch()) return rc;
-  if (p.nseg > 1) hipLaunchKernelGGL((cross_fwd_combine_kernel<T, DP>), dim3((unsigned)p.units), dim3(kThreads), 0, st, a, p, row_units(a), part);
+  if (d.shares) hipLaunchKernelGGL((cross_fwd_combine_kernel<T, DP>), dim3((unsigned)(d.rows * a.B), kWaves), dim3(2 * DP), 0, st, a, d, part);
   return check_launch();
 }
 
 template <typename T, int DP>
 static int bwd_t(const CrossArgs& a, hipStream_t st) {
-  const Plan p = rows_plan(a), k = keys_plan(a);
-  constexpr size_t lds = 4 * key_tile<T>() * DP * sizeof(T), klds = 2 * (64 * DP * sizeof(T) + 256);
+  const Deal d = rows_deal(a), k = keys_deal(a);
+  constexpr size_t lds = 4 * key_tile<T, DP>() * DP * sizeof(T), klds = 2 * (64 * DP * sizeof(T) + 256);
   if (const int rc = allow_dynamic_lds<cross_dq_kernel<T, DP>>(lds)) return rc;
   if (const int rc = allow_dynamic_lds<cross_dkv_kernel<T, DP>>(klds)) return rc;
   float* stat = static_cast<float*>(a.ws);
   float* part = stat + stat_bytes(a) / sizeof(float);
-  hipLaunchKernelGGL((cross_dq_kernel<T, DP>), dim3((unsigned)(p.units * p.nseg)), dim3(kThreads), lds, st, a, p, row_units(a), stat, part);
+  hipLaunchKernelGGL((cross_dq_kernel<T, DP>), dim3(d.grid), dim3(kThreads), lds, st, a, d, stat, part);
   if (const int rc = check_launch()) return rc;
-  if (p.nseg > 1) hipLaunchKernelGGL((cross_dq_combine_kernel<T, DP>), dim3((unsigned)p.units), dim3(kThreads), 0, st, a, p, row_units(a), part);
+  if (d.shares) hipLaunchKernelGGL((cross_dq_combine_kernel<T, DP>), dim3((unsigned)(d.rows * a.B), kWaves), dim3(2 * DP), 0, st, a, d, part);
   if (const int rc = check_launch()) return rc;
-  const int key_units = (a.S + kUnitRows - 1) / kUnitRows;
-  hipLaunchKernelGGL((cross_dkv_kernel<T, DP>), dim3((unsigned)(k.units * k.nseg), DP > 128 ? 2 : 1), dim3(kThreads), klds, st, a, k, key_units, stat, part);
+  hipLaunchKernelGGL((cross_dkv_kernel<T, DP>), dim3(k.grid, DP > 128 ? 2 : 1), dim3(kThreads), klds, st, a, k, stat, part);
   if (const int rc = check_launch()) return rc;
-  if (k.nseg > 1) hipLaunchKernelGGL((cross_dkv_combine_kernel<T, DP>), dim3((unsigned)k.units, 2), dim3(kThreads), 0, st, a, k, key_units, part);
+  hipLaunchKernelGGL((cross_dkv_combine_kernel<T, DP>), dim3((unsigned)(k.rows * a.B), kWaves, 2), dim3(2 * DP), 0, st, a, k, part);
   return check_launch();
 }
 
-int launch_cross_fwd(const CrossArgs& a, hipStream_t st) {
+// A tile's offsets fit 31 bits.
+static int is_near(const CrossArgs& a, bool backward) {
+  const int64_t most = 0x7fffffffLL / (64 * (a.dtype == BSA_F32 ? 4 : 2)) - a.d;
+  return a.k.l < most && a.v.l < most && (!backward || (a.q.l < most && a.go.l < most));
+}
+
+int launch_cross_fwd(const CrossArgs& given, hipStream_t st) {
+  CrossArgs a = given;
+  a.near = is_near(a, false);
   const bool f = a.dtype == BSA_F32;
   switch (padded_d(a.d)) {
     case 64: return f ? fwd_t<float, 64>(a, st) : fwd_t<uint16_t, 64>(a, st);
@@ -579,7 +742,9 @@ int launch_cross_fwd(const CrossArgs& a, hipStream_t st) {
   }
 }
 
-int launch_cross_bwd(const CrossArgs& a, hipStream_t st) {
+int launch_cross_bwd(const CrossArgs& given, hipStream_t st) {
+  CrossArgs a = given;
+  a.near = is_near(a, true);
   const bool f = a.dtype == BSA_F32;
   switch (padded_d(a.d)) {
     case 64: return f ? bwd_t<float, 64>(a, st) : bwd_t<uint16_t, 64>(a, st);
