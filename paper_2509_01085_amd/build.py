@@ -22,6 +22,7 @@ SOURCES = [
     "bsa_attn_dkv.hip",
     "bsa_qk_norm_rope.hip",
     "bsa_cross.hip",
+    "bsa_cross_dkv.hip",
     "bsa_probe.hip",
 ]
 # -ffp-contract=off: the decision kernels fix every rounding; packed-fp32 ops are disabled

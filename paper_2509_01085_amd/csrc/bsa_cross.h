@@ -26,6 +26,12 @@ __device__ inline Args* afresh(Args* a) {
   return a;
 }
 
+// A lane number that the compiler takes for a new one: what a piece of work computes from it is not kept for the next.
+__device__ inline int afresh(int lane) {
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+
 // ---- element types ----
 template <typename T> struct Elt;
 template <> struct Elt<uint16_t> {
@@ -166,7 +172,7 @@ struct Requests {
 struct Keys {
   int n;                 // valid length
   const uint8_t* mask;   // the batch entry's, or NULL
-  __device__ inline Keys(Args& a, int b) : n(a.kv_len ? max(0, min(a.kv_len[b], a.S)) : a.S), mask(a.kv_mask ? a.kv_mask + (int64_t)b * a.S : nullptr) {}
+  __device__ inline Keys(Args& a, int b) : n(a.kv_len ? __builtin_amdgcn_readfirstlane(max(0, min(a.kv_len[b], a.S))) : a.S), mask(a.kv_mask ? a.kv_mask + (int64_t)b * a.S : nullptr) {}
   __device__ inline uint64_t bits(int first, int count, int lane) const {
     if (!mask) {  // (uniform: a length alone)
       const int left = n - first;
@@ -222,5 +228,146 @@ __device__ inline void store_zeros(T* p, int d, int grp) {
       if (ch < d) store4(p + ch, f32x4{0.f, 0.f, 0.f, 0.f});
     }
 }
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+
+// ---- how a launch's work is dealt out ----
+// A unit (128 query rows of one key head; dK and dV: a tile of keys) takes a number of steps (key tiles; query tiles).  Either
+// every unit is a workgroup's, or all steps of a launch, unit after unit, are cut into equal shares: a workgroup's first and
+// last piece may then be parts of a unit, whose fp32 results it leaves for a second launch that adds them up in
+// order.  Shares keep the chip full where units are few, long or (valid lengths) unlike.
+struct Deal {
+  int grid;      // workgroups
+  int shares;    // 0: workgroup n takes unit n
+  int by_keys;   // units are tiles of `tile` keys and take `steps` steps; else `rows` units an entry of a step per `tile` valid keys
+  int tile, steps;
+  int64_t rows;  // units of a batch entry: (by_keys) of S keys
+};
+
+// A value that is the same in all lanes, in scalar registers.
+__device__ inline int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline int64_t same(int64_t v) { return (int64_t)uniform64((const void*)v); }
+
+struct Ledger {
+  const Deal& dl;
+  const int* len;
+  int B, S, Hkv, lane;
+  __device__ inline Ledger(Args& a, const Deal& dl_, int lane_) : dl(dl_), len(a.kv_len), B(a.B), S(a.S), Hkv(a.Hkv), lane(lane_) {}
+  __device__ inline int valid(int b) const { return len ? max(0, min(len[b], S)) : S; }  // b may differ from lane to lane
+  __device__ inline int tiles(int b) const { return (valid(b) + dl.tile - 1) / dl.tile; }
+  __device__ inline int steps(int b) const { return dl.by_keys ? dl.steps : tiles(b); }
+  __device__ inline int64_t units(int b) const { return dl.by_keys ? (int64_t)Hkv * tiles(b) : dl.rows; }  // that take steps
+  __device__ inline int64_t weight(int b) const { return units(b) * steps(b); }
+  __device__ inline int64_t scan(int64_t v) const {  // inclusive, over the lanes
+    const int lane = afresh(this->lane);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t w = __shfl_up(v, o);
+      if (lane >= o) v += w;
+    }
+    return v;
+  }
+  // Steps of the entries below b (of all with b = B).
+  __device__ inline int64_t below(int b) const {
+    if (!len) return b * weight(0);
+    int64_t sum = 0;
+    for (int b0 = 0; b0 < b; b0 += 64) sum += same(__shfl(scan(b0 + lane < b ? weight(b0 + lane) : 0), 63));
+    return sum;
+  }
+  // The entry that step `pos` is of, and the step that it begins with.
+  __device__ inline int entry(int64_t pos, int64_t& base) const {
+    if (!len) {
+      const int64_t w = weight(0);
+      const int b = (int)(pos / w);
+      base = b * w;
+      return b;
+    }
+    base = 0;
+    for (int b0 = 0;; b0 += 64) {
+      const int64_t v = b0 + lane < B ? weight(b0 + lane) : 0, to = scan(v);
+      const uint64_t past = __ballot(base + to > pos);
+      if (past || b0 + 64 >= B) {
+        const int l = __builtin_amdgcn_readfirstlane(__builtin_ctzll(past | (1ull << 63)));
+        base += same(__shfl(to - v, l));
+        return b0 + l;
+      }
+      base += same(__shfl(to, 63));
+    }
+  }
+};
+
+// One piece of a workgroup's work: steps t0 .. t1 - 1 of a unit.
+struct Piece {
+  int b, t0, t1;
+  int64_t unit;   // of the entry
+  int slot;       // of its partial results; -1: the unit is whole
+};
+
+template <typename F>
+__device__ inline void for_pieces(Args& a, const Deal& dl, int lane, F work) {
+  const Ledger led(a, dl, lane);
+  int64_t pos = 0, begin = 0, end = 1, per = 1;
+  if (dl.shares) {
+    const int64_t total = led.below(a.B);
+    per = (total + dl.grid - 1) / dl.grid;
+    begin = pos = blockIdx.x * per;
+    end = min(begin + per, total);
+  }
+  while (pos < end) {
+    Piece pc;
+    if (dl.shares) {
+      int64_t base;
+      pc.b = led.entry(pos, base);
+      const int steps = same(led.steps(pc.b));
+      pc.unit = (pos - base) / steps;
+      pc.t0 = (int)(pos - base - pc.unit * steps);
+      pc.t1 = (int)min((int64_t)steps, pc.t0 + (end - pos));
+      pc.slot = pc.t0 == 0 && pc.t1 == steps ? -1 : 2 * (int)blockIdx.x + (pos != begin);
+      pos += pc.t1 - pc.t0;
+    } else {
+      pc.b = (int)(blockIdx.x / dl.rows);
+      pc.unit = blockIdx.x - pc.b * dl.rows;
+      pc.t0 = 0;
+      pc.t1 = same(led.steps(pc.b));
+      pc.slot = -1;
+      pos = end;
+    }
+    work(pc);
+  }
+}
+
+// The partial results of a unit of entry b: how many there are (0: the unit is whole, -1: nobody worked on it) and their slots.
+struct Parts {
+  int n;
+  int64_t per, first, w0;
+  __device__ inline Parts(Args& a, const Deal& dl, int lane, int b, int64_t unit) : n(-1), per(0), first(0), w0(0) {
+    const Ledger led(a, dl, lane);
+    const int steps = led.steps(b);
+    if (steps == 0 || unit >= led.units(b)) return;
+    const int64_t total = led.below(a.B);
+    per = (total + dl.grid - 1) / dl.grid;
+    first = led.below(b) + unit * steps;
+    w0 = first / per;
+    n = (int)((first + steps - 1) / per - w0);
+    if (n) ++n;
+  }
+  __device__ inline int64_t slot(int k) const { return 2 * (w0 + k) + ((w0 + k) * per < first); }
+};
+
+// Partial results: [slot][wavefront][value][lane] floats.
+template <int VALUES>
+__device__ inline float* part_of(float* base, int64_t slot, int wave, int lane) {
+  return base + ((slot * kWaves + wave) * VALUES) * 64 + lane;
+}
+
+// The query tiles of dK and dV: 32 tokens of a head from first_token(i) on; where the last one would reach past Lq it begins
+// earlier and the tokens that it shares with its neighbour weigh nothing in it.
+__host__ __device__ inline int query_tiles(int Lq) { return (Lq + 31) / 32; }
+__host__ __device__ inline int first_token(int Lq, int i) { return Lq < 32 ? 0 : (32 * i < Lq - 32 ? 32 * i : Lq - 32); }
+
+// dK and dV of bf16 tensors with d <= 128 and Lq >= 32 (bsa_cross_dkv.hip); stat: the row statistics that the dQ launch left.
+size_t cross_dkv_fast_parts(const CrossArgs& a);
+int grant_cross_dkv_fast(const CrossArgs& a);  // before any launch of the call
+int launch_cross_dkv_fast(const CrossArgs& a, const float* stat, float* part, hipStream_t st);
 
 }  // namespace bsa

@@ -10,134 +10,9 @@
 
 namespace bsa {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kUnitRows = 32 * kWaves;
 
 template <typename T, int DP> constexpr int key_tile() { return sizeof(T) == 2 && DP <= 128 ? 64 : 32; }
-
-// ---- how a launch's work is dealt out ----
-// A unit (kUnitRows query rows of one key head; dK and dV: a tile of keys) takes a number of steps (key tiles; query tiles).  Either
-// every unit is a workgroup's, or all steps of a launch, unit after unit, are cut into equal shares: a workgroup's first and
-// last piece may then be parts of a unit, whose fp32 results it leaves for a second launch that adds them up in
-// order.  Shares keep the chip full where units are few, long or (valid lengths) unlike.
-struct Deal {
-  int grid;      // workgroups
-  int shares;    // 0: workgroup n takes unit n
-  int by_keys;   // units are tiles of `tile` keys and take `steps` steps; else `rows` units an entry of a step per `tile` valid keys
-  int tile, steps;
-  int64_t rows;  // units of a batch entry: (by_keys) of S keys
-};
-
-struct Ledger {
-  const Deal& dl;
-  const int* len;
-  int B, S, Hkv, lane;
-  __device__ inline Ledger(Args& a, const Deal& dl_, int lane_) : dl(dl_), len(a.kv_len), B(a.B), S(a.S), Hkv(a.Hkv), lane(lane_) {}
-  __device__ inline int valid(int b) const { return len ? max(0, min(len[b], S)) : S; }
-  __device__ inline int tiles(int b) const { return (valid(b) + dl.tile - 1) / dl.tile; }
-  __device__ inline int steps(int b) const { return dl.by_keys ? dl.steps : tiles(b); }
-  __device__ inline int64_t units(int b) const { return dl.by_keys ? (int64_t)Hkv * tiles(b) : dl.rows; }  // that take steps
-  __device__ inline int64_t weight(int b) const { return units(b) * steps(b); }
-  __device__ inline int64_t scan(int64_t v) const {  // inclusive, over the lanes
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t w = __shfl_up(v, o);
-      if (lane >= o) v += w;
-    }
-    return v;
-  }
-  // Steps of the entries below b (of all with b = B).
-  __device__ inline int64_t below(int b) const {
-    if (!len) return b * weight(0);
-    int64_t sum = 0;
-    for (int b0 = 0; b0 < b; b0 += 64) sum += __shfl(scan(b0 + lane < b ? weight(b0 + lane) : 0), 63);
-    return sum;
-  }
-  // The entry that step `pos` is of, and the step that it begins with.
-  __device__ inline int entry(int64_t pos, int64_t& base) const {
-    if (!len) {
-      const int64_t w = weight(0);
-      const int b = (int)(pos / w);
-      base = b * w;
-      return b;
-    }
-    base = 0;
-    for (int b0 = 0;; b0 += 64) {
-      const int64_t v = b0 + lane < B ? weight(b0 + lane) : 0, to = scan(v);
-      const uint64_t past = __ballot(base + to > pos);
-      if (past || b0 + 64 >= B) {
-        const int l = __builtin_amdgcn_readfirstlane(__builtin_ctzll(past | (1ull << 63)));
-        base += __shfl(to - v, l);
-        return b0 + l;
-      }
-      base += __shfl(to, 63);
-    }
-  }
-};
-
-// One piece of a workgroup's work: steps t0 .. t1 - 1 of a unit.
-struct Piece {
-  int b, t0, t1;
-  int64_t unit;   // of the entry
-  int slot;       // of its partial results; -1: the unit is whole
-};
-
-template <typename F>
-__device__ inline void for_pieces(Args& a, const Deal& dl, int lane, F work) {
-  const Ledger led(a, dl, lane);
-  int64_t pos = 0, begin = 0, end = 1, per = 1;
-  if (dl.shares) {
-    const int64_t total = led.below(a.B);
-    per = (total + dl.grid - 1) / dl.grid;
-    begin = pos = blockIdx.x * per;
-    end = min(begin + per, total);
-  }
-  while (pos < end) {
-    Piece pc;
-    if (dl.shares) {
-      int64_t base;
-      pc.b = led.entry(pos, base);
-      const int steps = led.steps(pc.b);
-      pc.unit = (pos - base) / steps;
-      pc.t0 = (int)(pos - base - pc.unit * steps);
-      pc.t1 = (int)min((int64_t)steps, pc.t0 + (end - pos));
-      pc.slot = pc.t0 == 0 && pc.t1 == steps ? -1 : 2 * (int)blockIdx.x + (pos != begin);
-      pos += pc.t1 - pc.t0;
-    } else {
-      pc.b = (int)(blockIdx.x / dl.rows);
-      pc.unit = blockIdx.x - pc.b * dl.rows;
-      pc.t0 = 0;
-      pc.t1 = led.steps(pc.b);
-      pc.slot = -1;
-      pos = end;
-    }
-    work(pc);
-  }
-}
-
-// The partial results of a unit of entry b: how many there are (0: the unit is whole, -1: nobody worked on it) and their slots.
-struct Parts {
-  int n;
-  int64_t per, first, w0;
-  __device__ inline Parts(Args& a, const Deal& dl, int lane, int b, int64_t unit) : n(-1), per(0), first(0), w0(0) {
-    const Ledger led(a, dl, lane);
-    const int steps = led.steps(b);
-    if (steps == 0 || unit >= led.units(b)) return;
-    const int64_t total = led.below(a.B);
-    per = (total + dl.grid - 1) / dl.grid;
-    first = led.below(b) + unit * steps;
-    w0 = first / per;
-    n = (int)((first + steps - 1) / per - w0);
-    if (n) ++n;
-  }
-  __device__ inline int64_t slot(int k) const { return 2 * (w0 + k) + ((w0 + k) * per < first); }
-};
-
-// Partial results: [slot][wavefront][value][lane] floats.
-template <int VALUES>
-__device__ inline float* part_of(float* base, int64_t slot, int wave, int lane) {
-  return base + ((slot * kWaves + wave) * VALUES) * 64 + lane;
-}
 
 struct RowUnit {
   int b, hk, m, g, l;  // batch entry, key head, row, its head in the group and token
@@ -409,19 +284,21 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_fwd_combine_kernel(CrossArgs,
 
 // ---- dQ ----
 // dQ^T += K^T dS^T over the key tiles, S^T and dP^T recomputed.  Ahead of the walk each wavefront forms delta of its rows and leaves
-// (LSE, -delta) for the other kernel: per head and 32 tokens [32] LSE log2(e), [32] -delta; tokens past the last
-// have LSE = +inf, i.e. weights of zero.
+// (LSE, -delta) for the other kernel: per head and query tile [32] LSE log2(e), [32] -delta; places that hold no token of the tile's
+// own have LSE = +inf, i.e. weights of zero.
 __device__ inline void put_stat(Args& a, const RowUnit& u, float* stat, float lse2, float delta, int grp) {
   if (grp != 0 || !u.live) return;
-  const int tiles = (a.Lq + 31) / 32;
-  float* at = stat + (((int64_t)u.b * a.H + u.head(a)) * tiles + (u.l >> 5)) * 64;
-  at[u.l & 31] = lse2;
-  at[32 + (u.l & 31)] = -delta;
-  if (u.l == a.Lq - 1)
-    for (int i = (u.l & 31) + 1; i < 32; ++i) {
-      at[i] = INFINITY;
-      at[32 + i] = 0.f;
-    }
+  const int i = u.l >> 5, first = first_token(a.Lq, i), r = u.l - first;
+  float* at = stat + (((int64_t)u.b * a.H + u.head(a)) * query_tiles(a.Lq) + i) * 64;
+  at[r] = lse2;
+  at[32 + r] = -delta;
+  if (u.l == a.Lq - 1) {  // the tile's other places weigh nothing
+    for (int k = 0; k < 32; ++k)
+      if (k > r || first + k < 32 * i) {
+        at[k] = INFINITY;
+        at[32 + k] = 0.f;
+      }
+  }
 }
 
 template <typename T, int DP>
@@ -546,7 +423,7 @@ __device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) 
  for_pieces(args, dl, lane, [&](const Piece& pc) {
   Args& a = *afresh(kernel_args());
   const float c = a.sm_scale * kLog2e;
-  const int tiles = (a.Lq + 31) / 32;  // of a head
+  const int tiles = query_tiles(a.Lq);  // of a head
   const KeyUnit u(a, pc.b, pc.unit, wave, lane);
   const Keys keys(a, u.b);
   raw_barrier();
@@ -566,11 +443,12 @@ __device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) 
     }
   const int t0 = pc.t0, t1 = work ? pc.t1 : t0;
   auto request = [&](int t) {
-    const int g = t / tiles, i = t - g * tiles, head = u.hk * a.G + g, left = a.Lq - 32 * i;
-    const uint64_t there = left >= 32 ? 0xffffffffull : (1ull << left) - 1;
+    const int g = t / tiles, i = t - g * tiles, head = u.hk * a.G + g;
+    const int64_t first = first_token(a.Lq, i);
+    const uint64_t there = a.Lq >= 32 ? 0xffffffffull : (1ull << a.Lq) - 1;
     uint8_t* at = smem + (t & 1) * STAGE;
-    const T* Q = static_cast<const T*>(a.Q) + u.b * a.q.b + (int64_t)head * a.q.h + (int64_t)32 * i * a.q.l;
-    const T* G = static_cast<const T*>(a.dO) + u.b * a.go.b + (int64_t)head * a.go.h + (int64_t)32 * i * a.go.l;
+    const T* Q = static_cast<const T*>(a.Q) + u.b * a.q.b + (int64_t)head * a.q.h + first * a.q.l;
+    const T* G = static_cast<const T*>(a.dO) + u.b * a.go.b + (int64_t)head * a.go.h + first * a.go.l;
     rq(at, Q, a.q.l, there, a.near);
     rg(at + TILE, G, a.go.l, there, a.near);
     if (tid < 16) dma16(stat + (((int64_t)u.b * a.H + head) * tiles + i) * 64 + 4 * tid, at + 2 * TILE);
@@ -671,13 +549,11 @@ static Deal rows_deal(const CrossArgs& a) {
   return d;
 }
 
-static int query_tiles(const CrossArgs& a) { return (a.Lq + 31) / 32; }  // of a head
-
 static Deal keys_deal(const CrossArgs& a) {
   Deal d{};
   d.by_keys = 1;
   d.tile = kUnitRows;
-  d.steps = a.G * query_tiles(a);
+  d.steps = a.G * query_tiles(a.Lq);
   d.rows = (int64_t)a.Hkv * ((a.S + kUnitRows - 1) / kUnitRows);
   const int64_t units = d.rows * a.B;
   d.shares = 1;
@@ -689,10 +565,16 @@ static size_t part_bytes(const Deal& d, int values) { return d.shares ? (size_t)
 
 size_t cross_fwd_workspace(const CrossArgs& a) { return part_bytes(rows_deal(a), padded_d(a.d) / 2 + 2); }
 
-static size_t stat_bytes(const CrossArgs& a) { return (size_t)a.B * a.H * query_tiles(a) * 256; }
+static size_t stat_bytes(const CrossArgs& a) { return (size_t)a.B * a.H * query_tiles(a.Lq) * 256; }
+
+// dK and dV on the kernel of bsa_cross_dkv.hip.  Below 32 tokens a head has no whole query tile.  (The strides may still ask for the
+// kernel here, so the workspace holds either's.)
+static bool fast_dkv(const CrossArgs& a) { return a.dtype == BSA_BF16 && a.d <= 128 && a.Lq >= 32; }
 
 size_t cross_bwd_workspace(const CrossArgs& a) {
-  return stat_bytes(a) + std::max(part_bytes(rows_deal(a), padded_d(a.d) / 2), part_bytes(keys_deal(a), padded_d(a.d)));
+  size_t parts = std::max(part_bytes(rows_deal(a), padded_d(a.d) / 2), part_bytes(keys_deal(a), padded_d(a.d)));
+  if (fast_dkv(a)) parts = std::max(parts, cross_dkv_fast_parts(a));
+  return stat_bytes(a) + parts;
 }
 
 template <typename T, int DP>
@@ -712,13 +594,15 @@ static int bwd_t(const CrossArgs& a, hipStream_t st) {
   const Deal d = rows_deal(a), k = keys_deal(a);
   constexpr size_t lds = 4 * key_tile<T, DP>() * DP * sizeof(T), klds = 2 * (64 * DP * sizeof(T) + 256);
   if (const int rc = allow_dynamic_lds<cross_dq_kernel<T, DP>>(lds)) return rc;
-  if (const int rc = allow_dynamic_lds<cross_dkv_kernel<T, DP>>(klds)) return rc;
+  const bool fast = fast_dkv(a) && a.near;
+  if (const int rc = fast ? grant_cross_dkv_fast(a) : allow_dynamic_lds<cross_dkv_kernel<T, DP>>(klds)) return rc;
   float* stat = static_cast<float*>(a.ws);
   float* part = stat + stat_bytes(a) / sizeof(float);
   hipLaunchKernelGGL((cross_dq_kernel<T, DP>), dim3(d.grid), dim3(kThreads), lds, st, a, d, stat, part);
   if (const int rc = check_launch()) return rc;
   if (d.shares) hipLaunchKernelGGL((cross_dq_combine_kernel<T, DP>), dim3((unsigned)(d.rows * a.B), kWaves), dim3(2 * DP), 0, st, a, d, part);
   if (const int rc = check_launch()) return rc;
+  if (fast) return launch_cross_dkv_fast(a, stat, part, st);
   hipLaunchKernelGGL((cross_dkv_kernel<T, DP>), dim3(k.grid, DP > 128 ? 2 : 1), dim3(kThreads), klds, st, a, k, stat, part);
   if (const int rc = check_launch()) return rc;
   hipLaunchKernelGGL((cross_dkv_combine_kernel<T, DP>), dim3((unsigned)(k.rows * a.B), kWaves, 2), dim3(2 * DP), 0, st, a, k, part);
