@@ -121,6 +121,36 @@ struct TileView {
   }
 };
 
+// The fragments of a bf16 tile by LDS byte offset, so that the tile's place folds into the instruction: AT is the tile's offset from
+// `base`.
+template <int D>
+struct Fragments {
+  static constexpr int RB = D * 2, DT = D / 32, DS = D / 16;
+  int koffs[DS], voffs[2][DT];
+  __device__ inline Fragments(uint32_t base, int lane) {
+    const int grp = lane >> 5, col = lane & 31;
+#pragma unroll
+    for (int s = 0; s < DS; ++s) koffs[s] = base + col * RB + (((2 * s + grp) ^ swz<D>(col)) << 4);
+    const int L16 = lane & 15, q16 = lane >> 4, rsub = L16 >> 2, jj = L16 & 3;
+    const int cl = 2 * (q16 & 1) + (jj >> 1), rhi = D == 128 ? rsub : (rsub >> 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        voffs[h][dt] = base + (8 * h + 4 * grp + rsub) * RB + ((((dt ^ rhi) << 2) | (cl ^ (2 * h + grp))) << 4) + 8 * (jj & 1);
+  }
+  __device__ inline void move(int by) {
+#pragma unroll
+    for (int s = 0; s < DS; ++s) koffs[s] += by;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) voffs[h][dt] += by;
+  }
+  template <int AT> __device__ inline bf16x8 row(int row0, int s) const { return frag_at(koffs[s] + AT + row0 * RB); }
+  template <int AT> __device__ inline bf16x8 along(int row0, int dt) const { return frag_tr_at(voffs[0][dt] + AT + row0 * RB, voffs[1][dt] + AT + row0 * RB); }
+};
+
 // What rows and channels that do not exist read instead.
 __device__ __constant__ const uint4 kZeroChunk = {0, 0, 0, 0};
 
@@ -131,13 +161,16 @@ struct Requests {
   using V = TileView<T, DP>;
   static constexpr int N = ROWS * V::CPR / NT;  // requests of a thread
   static_assert(ROWS * V::CPR % NT == 0, "whole requests");
-  uint32_t off[N];  // byte offsets from the tile's first row; not used unless they fit (near)
+  // Where an instruction's rows are a multiple of 16, the swizzle is the same for all and they differ by a scalar step.
+  static constexpr bool STEPS = NT / V::CPR % 16 == 0;
+  uint32_t off[STEPS ? 1 : N];  // byte offsets from the tile's first row; not used unless they fit (near)
+  int64_t step;
   int tid, d;
   __device__ inline int row(int n) const { return (n * NT + tid) / V::CPR; }
   __device__ inline int channel(int n) const { return (((n * NT + tid) % V::CPR) ^ tile_swz<T, DP>(row(n))) * V::E::CE; }
-  __device__ inline Requests(int64_t stride, int d_, int tid_) : tid(tid_), d(d_) {
+  __device__ inline Requests(int64_t stride, int d_, int tid_) : step(NT / V::CPR * stride * (int64_t)sizeof(T)), tid(tid_), d(d_) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) off[n] = (uint32_t)((row(n) * stride + channel(n)) * (int64_t)sizeof(T));
+    for (int n = 0; n < (STEPS ? 1 : N); ++n) off[n] = (uint32_t)((row(n) * stride + channel(n)) * (int64_t)sizeof(T));
   }
   __device__ inline void clear(uint8_t* tile) const {
 #pragma unroll
@@ -150,7 +183,10 @@ struct Requests {
     const uint32_t lds = uniform_lds(tile + (tid >> 6) * 1024);
 #pragma unroll
     for (int n = 0; n < N; ++n)
-      if (channel(n) < d) dma16_raw(sbase, off[n], lds + n * NT * 16);
+      if (channel(n) < d) {
+        if constexpr (STEPS) dma16_raw(sbase + n * step, off[0], lds + n * NT * 16);
+        else dma16_raw(sbase, off[n], lds + n * NT * 16);
+      }
   }
   // Rows whose bit in `there` is not set arrive as zeros.
   __device__ inline void some(uint8_t* tile, const T* base, int64_t stride, uint64_t there) const {

@@ -82,12 +82,12 @@ struct RowFrags {
   }
 };
 template <typename T, int DP> constexpr int two_a_cu() { return sizeof(T) == 2 && DP <= 128 ? 2 : 1; }
-template <typename T, int DP> constexpr bool held() { return DP * sizeof(T) <= 512; }  // one row beside an accumulator of DP channels
+template <typename T, int DP> constexpr bool held() { return DP <= 128; }
 
 // ---- forward ----
 // O = 0 and LSE = -inf without a valid key; a row whose valid logits are all -inf has no softmax and is NaN.
 __device__ inline void put_lse(Args& a, const RowUnit& u, float m, float l, bool any, int grp) {
-  if (grp == 0 && u.live) a.LSE_out[u.flat(a)] = any ? __builtin_fmaf(m, a.sm_scale, __builtin_amdgcn_logf(l) * kLn2) : -INFINITY;
+  if (grp == 0 && u.live) a.LSE_out[u.flat(a)] = any ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 template <typename T, int DT>
 __device__ inline void finish_row(Args& a, const RowUnit& u, const f32x16 (&acc)[DT], float m, float l, bool any, int grp) {
@@ -121,100 +121,169 @@ struct KvRing {
   static constexpr uint64_t ALL = KT == 64 ? ~0ull : (1ull << KT) - 1;
 };
 
+// A wavefront's state in the forward walk: O^T unnormalised, the running maximum (of the scaled logits, base 2; finite from the
+// start, so that logits of -inf weigh nothing wherever they stand) and the lane's share of the sum.
+constexpr float kLowest = -3.4e38f;
+template <int DT>
+struct Walked {
+  f32x16 o[DT];
+  float m = kLowest, l = 0.f;
+  __device__ inline Walked() {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+  }
+  // logits -> probabilities relative to the new maximum; what was gathered before is brought to it
+  template <int NK>
+  __device__ inline void softmax(f32x16 (&s)[NK], float c) {
+    float top = s[0][0];
+#pragma unroll
+    for (int k = 0; k < NK; ++k)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
+    const float next = fmaxf(m, pair_max(top) * c);  // c > 0: the maximum commutes with the scaling
+    const float f = __builtin_amdgcn_exp2f(m - next);
+    float sum[NK];
+#pragma unroll
+    for (int k = 0; k < NK; ++k) sum[k] = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        s[k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], c, -next));
+        sum[k] += s[k][r];
+      }
+    l = __builtin_fmaf(l, f, NK == 2 ? sum[0] + sum[NK - 1] : sum[0]);
+    m = next;
+    if (__builtin_amdgcn_ballot_w64(f != 1.f)) {  // only when some row's maximum moved
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+    }
+  }
+};
+
+// Logits of keys that are not valid, `own` being the tile's bits from the lane's first row on.
+template <int NK>
+__device__ inline void mask_logits(f32x16 (&s)[NK], uint64_t own) {
+#pragma unroll
+  for (int k = 0; k < NK; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (!((own >> (32 * k + d_row(r))) & 1)) s[k][r] = -INFINITY;
+}
+
+
+// One tile of 64 keys, bf16 and d <= 128: the LDS fragments of the tile (K, then V) run through a ring of RINGF registers
+// ahead of the products, in groups of two between which nothing moves.
+template <int D>
+__device__ inline void fwd_tile(Walked<D / 32>& w, const Fragments<D>& fg, const bf16x8* q, float c, uint64_t valid, int grp) {
+  constexpr int DT = D / 32, DS = D / 16, NF = 2 * DS + 4 * DT, TILE = 64 * D * 2, RINGF = 8;
+  auto frag = [&](auto F) -> bf16x8 {
+    constexpr int f = decltype(F)::value;
+    if constexpr (f < 2 * DS) return fg.template row<0>(32 * (f / DS), f % DS);
+    else return fg.template along<TILE>(16 * ((f - 2 * DS) / DT), (f - 2 * DS) % DT);
+  };
+  bf16x8 fr[RINGF];
+  static_for<0, RINGF>([&](auto F) { fr[decltype(F)::value] = frag(F); });
+  __builtin_amdgcn_sched_barrier(0);
+  f32x16 s[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[k][r] = 0.f;
+  static_for<0, 2 * DS>([&](auto F) {
+    constexpr int f = decltype(F)::value;
+    s[f / DS] = mfma32(fr[f % RINGF], q[f % DS], s[f / DS]);
+    if constexpr (f + RINGF < NF) fr[f % RINGF] = frag(std::integral_constant<int, f + RINGF>{});
+    if constexpr (f & 1) __builtin_amdgcn_sched_barrier(0);
+  });
+  if (valid != ~0ull) mask_logits<2>(s, valid >> (4 * grp));
+  w.template softmax<2>(s, c);
+  bf16x8 p[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p[k] = d_to_b(s[k >> 1], k & 1);
+  __builtin_amdgcn_sched_barrier(0);
+  static_for<2 * DS, NF>([&](auto F) {  // V^T in (key step, channel tile) order: neighbours hit different accumulators
+    constexpr int f = decltype(F)::value, v = f - 2 * DS;
+    w.o[v % DT] = mfma32(fr[f % RINGF], p[v / DT], w.o[v % DT]);
+    if constexpr (f + RINGF < NF) fr[f % RINGF] = frag(std::integral_constant<int, f + RINGF>{});
+    if constexpr (f & 1) __builtin_amdgcn_sched_barrier(0);
+  });
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_fwd_kernel(CrossArgs, Deal dl, float* part) {
   using E = Elt<T>;
   using Ring = KvRing<T, DP>;
   constexpr int KT = key_tile<T, DP>(), NK = KT / 32, DT = DP / 32;
   extern __shared__ __align__(16) uint8_t smem[];  // [2][K tile | V tile]
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 5;
-  const TileView<T, DP> view(lane);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Ring ring(smem, *kernel_args(), tid);
 
-  for_pieces(*kernel_args(), dl, lane, [&](const Piece& pc) {
+  for_pieces(*kernel_args(), dl, tid & 63, [&](const Piece& pc) {
     Args& a = *afresh(kernel_args());
+    const int lane = afresh(threadIdx.x & 63), grp = lane >> 5;
     const float c = a.sm_scale * kLog2e;
     const RowUnit u(a, pc.b, pc.unit, wave, lane);
     const Keys keys(a, u.b);
     raw_barrier();  // the ring is free
     uint64_t bits = pc.t0 < pc.t1 ? ring.request(a, u.b, u.hk, keys, pc.t0) : 0;
     const RowFrags<T, DP, held<T, DP>()> q(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
-    f32x16 o[DT];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    Walked<DT> w;
     bool any = false;
-    for (int t = pc.t0; t < pc.t1; ++t) {
-      wait_vm<0>();
-      raw_barrier();
-      const uint64_t now = bits;
-      if (t + 1 < pc.t1) bits = ring.request(a, u.b, u.hk, keys, t + 1);
-      if (now == 0 || !u.any) continue;
-      any = true;
-      const uint8_t* kt = ring.k_tile(t);
-      const uint8_t* vt = ring.v_tile(t);
-      f32x16 s[NK];
+    auto walk = [&](auto tile, auto past) {
+      for (int t = pc.t0; t < pc.t1; ++t) {
+        wait_vm<0>();
+        raw_barrier();
+        const uint64_t now = bits;
+        if (t + 1 < pc.t1) bits = ring.request(a, u.b, u.hk, keys, t + 1);
+        if (now != 0 && u.any) {
+          any = true;
+          tile(t, now);
+        }
+        past(t);
+      }
+    };
+    if constexpr (sizeof(T) == 2 && DP <= 128) {
+      Fragments<DP> fg(uniform_lds(smem) + (pc.t0 & 1) * 2 * Ring::TILE, lane);
+      walk([&](int t, uint64_t now) { fwd_tile<DP>(w, fg, q.f, c, now, grp); }, [&](int t) { fg.move(t & 1 ? -2 * Ring::TILE : 2 * Ring::TILE); });
+    } else {
+      const TileView<T, DP> view(lane);
+      walk([&](int t, uint64_t now) {
+        f32x16 s[NK];
 #pragma unroll
-      for (int k = 0; k < NK; ++k)
+        for (int k = 0; k < NK; ++k) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[k][r] = 0.f;
-#pragma unroll
-      for (int k = 0; k < NK; ++k) q.times(s[k], view, kt, 32 * k);
-      if (now != Ring::ALL) {
-        const uint64_t own = now >> (4 * grp);
+          for (int r = 0; r < 16; ++r) s[k][r] = 0.f;
+          q.times(s[k], view, ring.k_tile(t), 32 * k);
+        }
+        if (now != Ring::ALL) mask_logits<NK>(s, now >> (4 * grp));
+        w.template softmax<NK>(s, c);
 #pragma unroll
         for (int k = 0; k < NK; ++k)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!((own >> (32 * k + d_row(r))) & 1)) s[k][r] = -INFINITY;
-      }
-      float top = s[0][0];
+          for (int h = 0; h < 2; ++h) {
+            const auto p = E::column(s[k], h);
 #pragma unroll
-      for (int k = 0; k < NK; ++k)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
-      top = pair_max(top);
-      if (__any(top > m)) {
-        const float next = fmaxf(m, top);
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - next) * c);
-        m = next;
-        l *= f;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[dt][r] *= f;
-      }
-      const float base = m == -INFINITY ? 0.f : m * c;  // (all logits so far are -inf: they weigh nothing)
-#pragma unroll
-      for (int k = 0; k < NK; ++k)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], c, -base));
-          l += s[k][r];
-        }
-#pragma unroll
-      for (int k = 0; k < NK; ++k)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const auto p = E::column(s[k], h);
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) E::mma8(o[dt], view.along(vt, 32 * k + 16 * h, dt), p);
-        }
+            for (int dt = 0; dt < DT; ++dt) E::mma8(w.o[dt], view.along(ring.v_tile(t), 32 * k + 16 * h, dt), p);
+          }
+      }, [](int) {});
     }
     if (!u.any) return;
-    l = pair_sum(l);
+    const float l = pair_sum(w.l);
     if (pc.slot < 0) {
-      finish_row<T, DT>(a, u, o, m, l, any, grp);
+      finish_row<T, DT>(a, u, w.o, w.m, l, any, grp);
       return;
     }
     float* out = part_of<DT * 16 + 2>(part, pc.slot, wave, lane);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = o[dt][r];
-    out[DT * 16 * 64] = m;
+      for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = w.o[dt][r];
+    out[DT * 16 * 64] = w.m;
     out[(DT * 16 + 1) * 64] = any ? l : -1.f;  // (a sum is never negative)
   });
 }
@@ -257,20 +326,19 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_fwd_combine_kernel(CrossArgs,
   if (!u.any) return;
   const Parts ps(a, dl, lane, b, unit);
   if (ps.n == 0) return;
-  const float c = a.sm_scale * kLog2e;
   auto top_of = [&](int s) { return part_of<VALUES>(part, ps.slot(s), wave, lane)[DT * 16 * 64]; };
   auto sum_of = [&](int s) { return part_of<VALUES>(part, ps.slot(s), wave, lane)[(DT * 16 + 1) * 64]; };
-  float m = -INFINITY, l = 0.f;
+  float m = kLowest, l = 0.f;
   bool any = false;
 #pragma unroll 4
   for (int s = 0; s < ps.n; ++s) {
     const float ms = top_of(s), ls = sum_of(s);
     any |= ls != -1.f;
-    m = fmaxf(m, ls == -1.f ? -INFINITY : ms);
+    m = fmaxf(m, ls == -1.f ? kLowest : ms);
   }
   auto weight = [&](int s) {
     const float ms = top_of(s), ls = sum_of(s);
-    return ls == -1.f || (ms == -INFINITY && ls == 0.f) ? 0.f : __builtin_amdgcn_exp2f((ms - m) * c);
+    return ls == -1.f ? 0.f : __builtin_amdgcn_exp2f(ms - m);
   };
 #pragma unroll 4
   for (int s = 0; s < ps.n; ++s) {
@@ -301,18 +369,66 @@ __device__ inline void put_stat(Args& a, const RowUnit& u, float* stat, float ls
   }
 }
 
+// Probabilities of keys that are not valid.
+__device__ inline void mask_weights(f32x16& p, uint64_t own) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (!((own >> d_row(r)) & 1)) p[r] = 0.f;
+}
+
+// One tile of 64 keys, bf16 and d <= 128, 32 keys at a time: fragments as in fwd_tile, K and V rows in turn, then K^T.
+template <int D>
+__device__ inline void dq_tile(f32x16 (&dq)[D / 32], const Fragments<D>& fg, const bf16x8* q, const bf16x8* g, float c, float lse2, float delta,
+                               uint64_t valid, int grp) {
+  constexpr int DT = D / 32, DS = D / 16, NF = 2 * DS + 2 * DT, TILE = 64 * D * 2, RINGF = 4;
+  static_for<0, 2>([&](auto K) {
+    constexpr int k = decltype(K)::value;
+    auto frag = [&](auto F) -> bf16x8 {
+      constexpr int f = decltype(F)::value, v = f - 2 * DS;
+      if constexpr (f < 2 * DS) return fg.template row<(f & 1) * TILE>(32 * k, f >> 1);
+      else return fg.template along<0>(32 * k + 16 * (v / DT), v % DT);
+    };
+    bf16x8 fr[RINGF];
+    static_for<0, RINGF>([&](auto F) { fr[decltype(F)::value] = frag(F); });
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16 s, dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+    static_for<0, 2 * DS>([&](auto F) {
+      constexpr int f = decltype(F)::value;
+      if constexpr (f & 1) dp = mfma32(fr[f % RINGF], g[f >> 1], dp);
+      else s = mfma32(fr[f % RINGF], q[f >> 1], s);
+      if constexpr (f + RINGF < NF) fr[f % RINGF] = frag(std::integral_constant<int, f + RINGF>{});
+      if constexpr (f & 1) __builtin_amdgcn_sched_barrier(0);
+    });
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
+    if (valid != ~0ull) mask_weights(s, valid >> (32 * k + 4 * grp));
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+    const bf16x8 d0 = d_to_b(s, 0), d1 = d_to_b(s, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<2 * DS, NF>([&](auto F) {
+      constexpr int f = decltype(F)::value, v = f - 2 * DS;
+      dq[v % DT] = mfma32(fr[f % RINGF], v / DT ? d1 : d0, dq[v % DT]);
+      if constexpr (f + RINGF < NF) fr[f % RINGF] = frag(std::integral_constant<int, f + RINGF>{});
+      if constexpr (f & 1) __builtin_amdgcn_sched_barrier(0);
+    });
+  });
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel(CrossArgs, Deal dl, float* stat, float* part) {
   using E = Elt<T>;
   using Ring = KvRing<T, DP>;
   constexpr int KT = key_tile<T, DP>(), NK = KT / 32, DT = DP / 32;
   extern __shared__ __align__(16) uint8_t smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = lane >> 5;
-  const TileView<T, DP> view(lane);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Ring ring(smem, *kernel_args(), tid);
 
-  for_pieces(*kernel_args(), dl, lane, [&](const Piece& pc) {
+  for_pieces(*kernel_args(), dl, tid & 63, [&](const Piece& pc) {
     Args& a = *afresh(kernel_args());
+    const int lane = afresh(threadIdx.x & 63), grp = lane >> 5;
     const float c = a.sm_scale * kLog2e;
     const RowUnit u(a, pc.b, pc.unit, wave, lane);
     const Keys keys(a, u.b);
@@ -328,38 +444,43 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[dt][r] = 0.f;
-    for (int t = pc.t0; t < pc.t1; ++t) {
-      wait_vm<0>();
-      raw_barrier();
-      const uint64_t now = bits;
-      if (t + 1 < pc.t1) bits = ring.request(a, u.b, u.hk, keys, t + 1);
-      if (now == 0 || !u.any) continue;
-      const uint8_t* kt = ring.k_tile(t);
-      const uint8_t* vt = ring.v_tile(t);
-      const uint64_t own = now >> (4 * grp);
-#pragma unroll
-      for (int k = 0; k < NK; ++k) {
-        __builtin_amdgcn_sched_barrier(0);  // one half at a time in the registers
-        f32x16 s, dp;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
-        q.times(s, view, kt, 32 * k);
-        gr.times(dp, view, vt, 32 * k);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
-        if (now != Ring::ALL)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!((own >> (32 * k + d_row(r))) & 1)) s[r] = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const auto ds = E::column(s, h);
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) E::mma8(dq[dt], view.along(kt, 32 * k + 16 * h, dt), ds);
-        }
+    auto walk = [&](auto tile, auto past) {
+      for (int t = pc.t0; t < pc.t1; ++t) {
+        wait_vm<0>();
+        raw_barrier();
+        const uint64_t now = bits;
+        if (t + 1 < pc.t1) bits = ring.request(a, u.b, u.hk, keys, t + 1);
+        if (now != 0 && u.any) tile(t, now);
+        past(t);
       }
+    };
+    if constexpr (sizeof(T) == 2 && DP <= 128) {
+      Fragments<DP> fg(uniform_lds(smem) + (pc.t0 & 1) * 2 * Ring::TILE, lane);
+      walk([&](int t, uint64_t now) { dq_tile<DP>(dq, fg, q.f, gr.f, c, lse2, delta, now, grp); },
+           [&](int t) { fg.move(t & 1 ? -2 * Ring::TILE : 2 * Ring::TILE); });
+    } else {
+      const TileView<T, DP> view(lane);
+      walk([&](int t, uint64_t now) {
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+          f32x16 s, dp;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+          q.times(s, view, ring.k_tile(t), 32 * k);
+          gr.times(dp, view, ring.v_tile(t), 32 * k);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
+          if (now != Ring::ALL) mask_weights(s, now >> (32 * k + 4 * grp));
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const auto ds = E::column(s, h);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) E::mma8(dq[dt], view.along(ring.k_tile(t), 32 * k + 16 * h, dt), ds);
+          }
+        }
+      }, [](int) {});
     }
     if (!u.any) return;
     if (pc.slot < 0) {
