@@ -268,13 +268,17 @@ __device__ inline void store_zeros(T* p, int d, int grp) {
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 // ---- how a launch's work is dealt out ----
-// A unit (128 query rows of one key head; dK and dV: a tile of keys) takes a number of steps (key tiles; query tiles).  Either
-// every unit is a workgroup's, or all steps of a launch, unit after unit, are cut into equal shares: a workgroup's first and
-// last piece may then be parts of a unit, whose fp32 results it leaves for a second launch that adds them up in
-// order.  Shares keep the chip full where units are few, long or (valid lengths) unlike.
+// A unit (128 query rows of one key head; dK and dV: a tile of keys) takes a number of steps (key tiles; query tiles).
+//   EACH    workgroup n takes unit n;
+//   SHARES  all steps of a launch, unit after unit, are cut into equal shares: a workgroup's first and last piece may then
+//           be parts of a unit, whose fp32 results it leaves for a second launch that adds them up in order.  Keeps the chip
+//           full where units are few, long or (valid lengths) unlike.
+// (Runs of whole units, dealt out ahead of time, were slower than the hardware's handing out of single ones: 33,280 rows, 12 heads,
+// 512 keys, forward 151 and 159 us.)
+enum { EACH = 0, SHARES = 1 };
 struct Deal {
   int grid;      // workgroups
-  int shares;    // 0: workgroup n takes unit n
+  int way;
   int by_keys;   // units are tiles of `tile` keys and take `steps` steps; else `rows` units an entry of a step per `tile` valid keys
   int tile, steps;
   int64_t rows;  // units of a batch entry: (by_keys) of S keys
@@ -310,7 +314,7 @@ struct Ledger {
     for (int b0 = 0; b0 < b; b0 += 64) sum += same(__shfl(scan(b0 + lane < b ? weight(b0 + lane) : 0), 63));
     return sum;
   }
-  // The entry that step `pos` is of, and the step that it begins with.
+  // The entry that `pos` is of, and where it begins.
   __device__ inline int entry(int64_t pos, int64_t& base) const {
     if (!len) {
       const int64_t w = weight(0);
@@ -339,38 +343,55 @@ struct Piece {
   int slot;       // of its partial results; -1: the unit is whole
 };
 
-template <typename F>
-__device__ inline void for_pieces(Args& a, const Deal& dl, int lane, F work) {
-  const Ledger led(a, dl, lane);
-  int64_t pos = 0, begin = 0, end = 1, per = 1;
-  if (dl.shares) {
-    const int64_t total = led.below(a.B);
-    per = (total + dl.grid - 1) / dl.grid;
-    begin = pos = blockIdx.x * per;
-    end = min(begin + per, total);
-  }
-  while (pos < end) {
-    Piece pc;
-    if (dl.shares) {
-      int64_t base;
-      pc.b = led.entry(pos, base);
-      const int steps = same(led.steps(pc.b));
-      pc.unit = (pos - base) / steps;
-      pc.t0 = (int)(pos - base - pc.unit * steps);
-      pc.t1 = (int)min((int64_t)steps, pc.t0 + (end - pos));
-      pc.slot = pc.t0 == 0 && pc.t1 == steps ? -1 : 2 * (int)blockIdx.x + (pos != begin);
-      pos += pc.t1 - pc.t0;
-    } else {
-      pc.b = (int)(blockIdx.x / dl.rows);
-      pc.unit = blockIdx.x - pc.b * dl.rows;
-      pc.t0 = 0;
-      pc.t1 = same(led.steps(pc.b));
-      pc.slot = -1;
-      pos = end;
+// A workgroup's pieces, one after the other.  ONE: EACH, so there is one.
+template <bool ONE>
+struct Dealer {
+  const Ledger led;
+  int64_t pos, end, units, unit;
+  int b, t, steps;
+  bool fresh;  // no piece taken yet
+  __device__ inline Dealer(Args& a, const Deal& dl, int lane) : led(a, dl, lane), t(0), fresh(true) {
+    if constexpr (ONE) {
+      b = dl.rows == 1 ? blockIdx.x : blockIdx.x / (uint32_t)dl.rows;  // (units of a launch: less than 2^31)
+      unit = blockIdx.x - (uint32_t)b * (uint32_t)dl.rows;
+      steps = same(led.steps(b));
+      return;
     }
-    work(pc);
+    const int64_t total = led.below(a.B), per = (total + dl.grid - 1) / dl.grid;
+    pos = blockIdx.x * per;
+    end = min(pos + per, total);
+    if (pos >= end) return;
+    const int64_t base = enter();
+    unit = (pos - base) / steps;
+    t = (int)(pos - base - unit * steps);
   }
-}
+  __device__ inline int64_t enter() {
+    int64_t base;
+    b = led.entry(pos, base);
+    steps = same(led.steps(b));
+    units = same(led.units(b));
+    unit = 0;
+    return base;
+  }
+  __device__ inline bool next(Piece& pc) {
+    if constexpr (ONE) {
+      pc = Piece{b, 0, steps, unit, -1};
+      return true;
+    }
+    if (pos >= end) return false;
+    if (unit >= units) enter();
+    pc.b = b;
+    pc.unit = unit;
+    pc.t0 = t;
+    pc.t1 = (int)min((int64_t)steps, t + (end - pos));
+    pc.slot = t == 0 && pc.t1 == steps ? -1 : 2 * (int)blockIdx.x + !fresh;
+    pos += pc.t1 - t;
+    t = 0;  // (a share ends in a unit's middle or goes on with the next unit)
+    ++unit;
+    fresh = false;
+    return true;
+  }
+};
 
 // The partial results of a unit of entry b: how many there are (0: the unit is whole, -1: nobody worked on it) and their slots.
 struct Parts {
@@ -379,7 +400,7 @@ struct Parts {
   __device__ inline Parts(Args& a, const Deal& dl, int lane, int b, int64_t unit) : n(-1), per(0), first(0), w0(0) {
     const Ledger led(a, dl, lane);
     const int steps = led.steps(b);
-    if (steps == 0 || unit >= led.units(b)) return;
+    if (dl.way != SHARES || steps == 0 || unit >= led.units(b)) return;
     const int64_t total = led.below(a.B);
     per = (total + dl.grid - 1) / dl.grid;
     first = led.below(b) + unit * steps;

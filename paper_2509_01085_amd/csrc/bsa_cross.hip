@@ -32,6 +32,8 @@ struct RowUnit {
   __device__ inline int64_t flat(Args& a) const { return ((int64_t)b * a.H + head(a)) * a.Lq + l; }
 };
 
+__device__ inline int key_head(Args& a, int64_t unit) { return (int)(unit / ((a.M + kUnitRows - 1) / kUnitRows)); }
+
 // Chunk c of a row, zeros where there is none.
 template <typename T>
 __device__ inline typename Elt<T>::Frag row_chunk(const T* p, int c, bool live, int d) {
@@ -49,13 +51,19 @@ struct RowFrags {
   bool live;
   int d, grp;
   typename E::Frag f[HELD ? DS : 1];
-  __device__ inline RowFrags(const T* p_, bool live_, int d_, int grp_) : p(p_), live(live_), d(d_), grp(grp_) {
-    if constexpr (HELD) {
+  __device__ inline void load(const T* p_, bool live_, int d_, int grp_) {
+    p = p_;
+    live = live_;
+    d = d_;
+    grp = grp_;
+    if constexpr (HELD)
 #pragma unroll
       for (int s = 0; s < DS; ++s) f[s] = row_chunk(p, 2 * s + grp, live, d);
+  }
+  __device__ inline void arrive() {  // waited for here, not between a tile's requests and its products
+    if constexpr (HELD)
 #pragma unroll
-      for (int s = 0; s < DS; ++s) settle(f[s]);  // waited for here, not behind the first tile's requests
-    }
+      for (int s = 0; s < DS; ++s) settle(f[s]);
   }
   // D += rows row0 .. row0 + 31 of the tile times this
   __device__ inline void times(f32x16& acc, const TileView<T, DP>& view, const uint8_t* tile, int row0) const {
@@ -106,14 +114,14 @@ struct KvRing {
     if (a.d < DP)
       for (int k = 0; k < 4; ++k) rk.clear(smem + k * TILE);
   }
-  __device__ inline const uint8_t* k_tile(int t) const { return smem + (t & 1) * 2 * TILE; }
-  __device__ inline const uint8_t* v_tile(int t) const { return k_tile(t) + TILE; }
-  // returns the valid keys of tile t
-  __device__ inline uint64_t request(Args& a, int b, int hk, const Keys& keys, int t) const {
-    const uint64_t there = keys.bits(t * KT, KT, lane);
+  __device__ inline const uint8_t* k_tile(int place) const { return smem + place * 2 * TILE; }
+  __device__ inline const uint8_t* v_tile(int place) const { return k_tile(place) + TILE; }
+  // Tile t of key head hk into a place of the ring; returns its valid keys.
+  __device__ inline uint64_t request(Args& a, int b, int hk, int t, int place) const {
+    const uint64_t there = Keys(a, b).bits(t * KT, KT, lane);
     const T* K = static_cast<const T*>(a.K) + b * a.k.b + hk * a.k.h + (int64_t)t * KT * a.k.l;
     const T* V = static_cast<const T*>(a.V) + b * a.v.b + hk * a.v.h + (int64_t)t * KT * a.v.l;
-    uint8_t* at = smem + (t & 1) * 2 * TILE;
+    uint8_t* at = smem + place * 2 * TILE;
     rk(at, K, a.k.l, there, a.near);
     rv(at + TILE, V, a.v.l, there, a.near);
     return there;
@@ -121,9 +129,42 @@ struct KvRing {
   static constexpr uint64_t ALL = KT == 64 ? ~0ull : (1ull << KT) - 1;
 };
 
+// A workgroup's walk over its pieces and their tiles.  While a tile is multiplied the next one is on its way, be it this piece's or the
+// next one's: `place` is the multiplied tile's, the other one the requested tile's.
+template <typename T, int DP>
+struct Walk {
+  const KvRing<T, DP>& ring;
+  int place = 0;
+  bool asked = false;  // the coming piece's first tile has been requested
+  uint64_t bits = 0;   // its valid keys
+  __device__ inline explicit Walk(const KvRing<T, DP>& r) : ring(r) {}
+  // tile(place, valid keys) for every tile of a piece; past(place) behind it.  (No tile is passed over: a way round the products
+  // would have the compiler move the accumulators at every tile.)
+  template <typename F, typename G>
+  __device__ inline void operator()(Args& a, const Piece& pc, int hk, bool more, const Piece& nx, int next_hk, F tile, G past) {
+    if (!asked && pc.t0 < pc.t1) bits = ring.request(a, pc.b, hk, pc.t0, place);
+    asked = false;
+    for (int t = pc.t0; t < pc.t1; ++t) {
+      wait_vm<0>();
+      raw_barrier();  // the tile is there for all, and all are done with the other place
+      const uint64_t now = bits;
+      if (t + 1 < pc.t1) {
+        bits = ring.request(a, pc.b, hk, t + 1, place ^ 1);
+      } else if (more && nx.t0 < nx.t1) {
+        bits = ring.request(a, nx.b, next_hk, nx.t0, place ^ 1);
+        asked = true;
+      }
+      tile(place, now);
+      past(place);
+      place ^= 1;
+    }
+  }
+};
+
 // A wavefront's state in the forward walk: O^T unnormalised, the running maximum (of the scaled logits, base 2; finite from the
 // start, so that logits of -inf weigh nothing wherever they stand) and the lane's share of the sum.
 constexpr float kLowest = -3.4e38f;
+constexpr float kLag = 6.f;  // (base 2)
 template <int DT>
 struct Walked {
   f32x16 o[DT];
@@ -134,7 +175,8 @@ struct Walked {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
   }
-  // logits -> probabilities relative to the new maximum; what was gathered before is brought to it
+  // Logits -> probabilities relative to the row's maximum.  The maximum is moved, and what was gathered before brought to it, only where
+  // a logit exceeds it by kLag: with 32 rows a wavefront and few tiles one of them would move at nearly every tile.
   template <int NK>
   __device__ inline void softmax(f32x16 (&s)[NK], float c) {
     float top = s[0][0];
@@ -142,8 +184,16 @@ struct Walked {
     for (int k = 0; k < NK; ++k)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
-    const float next = fmaxf(m, pair_max(top) * c);  // c > 0: the maximum commutes with the scaling
-    const float f = __builtin_amdgcn_exp2f(m - next);
+    if (__builtin_amdgcn_ballot_w64(top * c > m + kLag)) {  // c > 0: the maximum commutes with the scaling
+      const float next = fmaxf(m, pair_max(top) * c);
+      const float f = __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+    }
     float sum[NK];
 #pragma unroll
     for (int k = 0; k < NK; ++k) sum[k] = 0.f;
@@ -151,17 +201,11 @@ struct Walked {
     for (int r = 0; r < 16; ++r)
 #pragma unroll
       for (int k = 0; k < NK; ++k) {
-        s[k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], c, -next));
+        s[k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], c, -m));
         sum[k] += s[k][r];
       }
-    l = __builtin_fmaf(l, f, NK == 2 ? sum[0] + sum[NK - 1] : sum[0]);
-    m = next;
-    if (__builtin_amdgcn_ballot_w64(f != 1.f)) {  // only when some row's maximum moved
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[dt][r] *= f;
-    }
+    for (int k = 0; k < NK; ++k) l += sum[k];
   }
 };
 
@@ -214,7 +258,8 @@ __device__ inline void fwd_tile(Walked<D / 32>& w, const Fragments<D>& fg, const
   });
 }
 
-template <typename T, int DP>
+// ONE: a unit a workgroup (Deal::EACH), without what the walk over several pieces needs.
+template <typename T, int DP, bool ONE>
 __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_fwd_kernel(CrossArgs, Deal dl, float* part) {
   using E = Elt<T>;
   using Ring = KvRing<T, DP>;
@@ -222,70 +267,80 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_fwd_kerne
   extern __shared__ __align__(16) uint8_t smem[];  // [2][K tile | V tile]
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Ring ring(smem, *kernel_args(), tid);
-
-  for_pieces(*kernel_args(), dl, tid & 63, [&](const Piece& pc) {
+  Walk<T, DP> walk(ring);
+  Dealer<ONE> dealer(*kernel_args(), dl, tid & 63);
+  Piece pc, nx;
+  if (!dealer.next(pc)) return;
+  using Rows = RowFrags<T, DP, held<T, DP>()>;
+  Rows q;
+  auto load_q = [&](Rows& to, Args& a, const Piece& p, int lane) {
+    const RowUnit u(a, p.b, p.unit, wave, lane);
+    to.load(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, lane >> 5);
+  };
+  load_q(q, *kernel_args(), pc, tid & 63);
+  for (;;) {
     Args& a = *afresh(kernel_args());
     const int lane = afresh(threadIdx.x & 63), grp = lane >> 5;
     const float c = a.sm_scale * kLog2e;
+    const bool more = !ONE && dealer.next(nx);
+    q.arrive();
     const RowUnit u(a, pc.b, pc.unit, wave, lane);
-    const Keys keys(a, u.b);
-    raw_barrier();  // the ring is free
-    uint64_t bits = pc.t0 < pc.t1 ? ring.request(a, u.b, u.hk, keys, pc.t0) : 0;
-    const RowFrags<T, DP, held<T, DP>()> q(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
     Walked<DT> w;
     bool any = false;
-    auto walk = [&](auto tile, auto past) {
-      for (int t = pc.t0; t < pc.t1; ++t) {
-        wait_vm<0>();
-        raw_barrier();
-        const uint64_t now = bits;
-        if (t + 1 < pc.t1) bits = ring.request(a, u.b, u.hk, keys, t + 1);
-        if (now != 0 && u.any) {
-          any = true;
-          tile(t, now);
-        }
-        past(t);
-      }
-    };
     if constexpr (sizeof(T) == 2 && DP <= 128) {
-      Fragments<DP> fg(uniform_lds(smem) + (pc.t0 & 1) * 2 * Ring::TILE, lane);
-      walk([&](int t, uint64_t now) { fwd_tile<DP>(w, fg, q.f, c, now, grp); }, [&](int t) { fg.move(t & 1 ? -2 * Ring::TILE : 2 * Ring::TILE); });
+      Fragments<DP> fg(uniform_lds(smem) + walk.place * 2 * Ring::TILE, lane);
+      auto skip = [&](int, uint64_t now) { any |= now != 0; };
+      if (!u.any) walk(a, pc, u.hk, more, nx, key_head(a, nx.unit), skip, [](int) {});
+      else walk(a, pc, u.hk, more, nx, key_head(a, nx.unit),
+                [&](int, uint64_t now) {
+                  any |= now != 0;
+                  fwd_tile<DP>(w, fg, q.f, c, now, grp);
+                },
+                [&](int place) { fg.move(place ? -2 * Ring::TILE : 2 * Ring::TILE); });
     } else {
       const TileView<T, DP> view(lane);
-      walk([&](int t, uint64_t now) {
-        f32x16 s[NK];
+      walk(a, pc, u.hk, more, nx, key_head(a, nx.unit),
+           [&](int place, uint64_t now) {
+             any |= now != 0;
+             if (!u.any || now == 0) return;
+             f32x16 s[NK];
 #pragma unroll
-        for (int k = 0; k < NK; ++k) {
+             for (int k = 0; k < NK; ++k) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[k][r] = 0.f;
-          q.times(s[k], view, ring.k_tile(t), 32 * k);
-        }
-        if (now != Ring::ALL) mask_logits<NK>(s, now >> (4 * grp));
-        w.template softmax<NK>(s, c);
+               for (int r = 0; r < 16; ++r) s[k][r] = 0.f;
+               q.times(s[k], view, ring.k_tile(place), 32 * k);
+             }
+             if (now != Ring::ALL) mask_logits<NK>(s, now >> (4 * grp));
+             w.template softmax<NK>(s, c);
 #pragma unroll
-        for (int k = 0; k < NK; ++k)
+             for (int k = 0; k < NK; ++k)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const auto p = E::column(s[k], h);
+               for (int h = 0; h < 2; ++h) {
+                 const auto p = E::column(s[k], h);
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) E::mma8(w.o[dt], view.along(ring.v_tile(t), 32 * k + 16 * h, dt), p);
-          }
-      }, [](int) {});
+                 for (int dt = 0; dt < DT; ++dt) E::mma8(w.o[dt], view.along(ring.v_tile(place), 32 * k + 16 * h, dt), p);
+               }
+           },
+           [](int) {});
     }
-    if (!u.any) return;
-    const float l = pair_sum(w.l);
-    if (pc.slot < 0) {
-      finish_row<T, DT>(a, u, w.o, w.m, l, any, grp);
-      return;
+    if (u.any) {
+      const float l = pair_sum(w.l);
+      if (pc.slot < 0) {
+        finish_row<T, DT>(a, u, w.o, w.m, l, any, grp);
+      } else {
+        float* out = part_of<DT * 16 + 2>(part, pc.slot, wave, lane);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = w.o[dt][r];
+        out[DT * 16 * 64] = w.m;
+        out[(DT * 16 + 1) * 64] = any ? l : -1.f;  // (a sum is never negative)
+      }
     }
-    float* out = part_of<DT * 16 + 2>(part, pc.slot, wave, lane);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = w.o[dt][r];
-    out[DT * 16 * 64] = w.m;
-    out[(DT * 16 + 1) * 64] = any ? l : -1.f;  // (a sum is never negative)
-  });
+    if (!more) return;
+    pc = nx;
+    load_q(q, a, pc, lane);
+  }
 }
 
 // Sum over the parts of a unit of the 16 values that a wavefront's channel tile has at `at` (values before it), each part times its
@@ -417,7 +472,7 @@ __device__ inline void dq_tile(f32x16 (&dq)[D / 32], const Fragments<D>& fg, con
   });
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool ONE>
 __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel(CrossArgs, Deal dl, float* stat, float* part) {
   using E = Elt<T>;
   using Ring = KvRing<T, DP>;
@@ -425,74 +480,74 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Ring ring(smem, *kernel_args(), tid);
-
-  for_pieces(*kernel_args(), dl, tid & 63, [&](const Piece& pc) {
+  Walk<T, DP> walk(ring);
+  Dealer<ONE> dealer(*kernel_args(), dl, tid & 63);
+  Piece pc, nx;
+  bool more = dealer.next(nx);
+  while (more) {
+    pc = nx;
     Args& a = *afresh(kernel_args());
     const int lane = afresh(threadIdx.x & 63), grp = lane >> 5;
     const float c = a.sm_scale * kLog2e;
     const RowUnit u(a, pc.b, pc.unit, wave, lane);
-    const Keys keys(a, u.b);
-    raw_barrier();
-    uint64_t bits = pc.t0 < pc.t1 ? ring.request(a, u.b, u.hk, keys, pc.t0) : 0;
-    const RowFrags<T, DP, held<T, DP>()> q(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
-    const RowFrags<T, DP, DP <= 128> gr(static_cast<const T*>(a.dO) + u.offset(a, a.go), u.live, a.d, grp);
+    RowFrags<T, DP, held<T, DP>()> q;
+    RowFrags<T, DP, held<T, DP>()> gr;
+    q.load(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
+    gr.load(static_cast<const T*>(a.dO) + u.offset(a, a.go), u.live, a.d, grp);
     const float delta = pair_sum(gr.dot(static_cast<const T*>(a.O) + u.offset(a, a.o)));
     const float lse2 = u.live ? a.LSE_in[u.flat(a)] * kLog2e : INFINITY;
+    more = !ONE && dealer.next(nx);
     if (pc.t0 == 0) put_stat(a, u, stat, lse2, delta, grp);
+    q.arrive();
+    gr.arrive();
     f32x16 dq[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[dt][r] = 0.f;
-    auto walk = [&](auto tile, auto past) {
-      for (int t = pc.t0; t < pc.t1; ++t) {
-        wait_vm<0>();
-        raw_barrier();
-        const uint64_t now = bits;
-        if (t + 1 < pc.t1) bits = ring.request(a, u.b, u.hk, keys, t + 1);
-        if (now != 0 && u.any) tile(t, now);
-        past(t);
-      }
-    };
     if constexpr (sizeof(T) == 2 && DP <= 128) {
-      Fragments<DP> fg(uniform_lds(smem) + (pc.t0 & 1) * 2 * Ring::TILE, lane);
-      walk([&](int t, uint64_t now) { dq_tile<DP>(dq, fg, q.f, gr.f, c, lse2, delta, now, grp); },
-           [&](int t) { fg.move(t & 1 ? -2 * Ring::TILE : 2 * Ring::TILE); });
+      Fragments<DP> fg(uniform_lds(smem) + walk.place * 2 * Ring::TILE, lane);
+      if (!u.any) walk(a, pc, u.hk, more, nx, key_head(a, nx.unit), [](int, uint64_t) {}, [](int) {});
+      else walk(a, pc, u.hk, more, nx, key_head(a, nx.unit), [&](int, uint64_t now) { dq_tile<DP>(dq, fg, q.f, gr.f, c, lse2, delta, now, grp); },
+                [&](int place) { fg.move(place ? -2 * Ring::TILE : 2 * Ring::TILE); });
     } else {
       const TileView<T, DP> view(lane);
-      walk([&](int t, uint64_t now) {
+      walk(a, pc, u.hk, more, nx, key_head(a, nx.unit),
+           [&](int place, uint64_t now) {
+             if (!u.any || now == 0) return;
 #pragma unroll
-        for (int k = 0; k < NK; ++k) {
-          f32x16 s, dp;
+             for (int k = 0; k < NK; ++k) {
+               f32x16 s, dp;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
-          q.times(s, view, ring.k_tile(t), 32 * k);
-          gr.times(dp, view, ring.v_tile(t), 32 * k);
+               for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+               q.times(s, view, ring.k_tile(place), 32 * k);
+               gr.times(dp, view, ring.v_tile(place), 32 * k);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
-          if (now != Ring::ALL) mask_weights(s, now >> (32 * k + 4 * grp));
+               for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
+               if (now != Ring::ALL) mask_weights(s, now >> (32 * k + 4 * grp));
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+               for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const auto ds = E::column(s, h);
+               for (int h = 0; h < 2; ++h) {
+                 const auto ds = E::column(s, h);
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) E::mma8(dq[dt], view.along(ring.k_tile(t), 32 * k + 16 * h, dt), ds);
-          }
-        }
-      }, [](int) {});
+                 for (int dt = 0; dt < DT; ++dt) E::mma8(dq[dt], view.along(ring.k_tile(place), 32 * k + 16 * h, dt), ds);
+               }
+             }
+           },
+           [](int) {});
     }
-    if (!u.any) return;
+    if (!u.any) continue;
     if (pc.slot < 0) {
       store_column<T, DT>(static_cast<T*>(a.dQ) + u.offset(a, a.gq), dq, a.sm_scale, a.d, grp, u.live);
-      return;
+    } else {
+      float* out = part_of<DT * 16>(part, pc.slot, wave, lane);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = dq[dt][r];
     }
-    float* out = part_of<DT * 16>(part, pc.slot, wave, lane);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) out[(dt * 16 + r) * 64] = dq[dt][r];
-  });
+  }
 }
 
 template <typename T, int DP>
@@ -541,7 +596,9 @@ __device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) 
   const Requests<T, DP, 32, kThreads> rq(args.q.l, args.d, tid), rg(args.go.l, args.d, tid);
   if (args.d < DP)
     for (int k = 0; k < 4; ++k) rq.clear(smem + (k >> 1) * STAGE + (k & 1) * TILE);
- for_pieces(args, dl, lane, [&](const Piece& pc) {
+ Dealer<false> dealer(args, dl, lane);
+ Piece pc;
+ while (dealer.next(pc)) {
   Args& a = *afresh(kernel_args());
   const float c = a.sm_scale * kLog2e;
   const int tiles = query_tiles(a.Lq);  // of a head
@@ -553,7 +610,11 @@ __device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) 
   const bool work = __syncthreads_or(mine != 0);                                   // of the workgroup
   const T* K = static_cast<const T*>(a.K) + u.b * a.k.b + u.hk * a.k.h + u.key * a.k.l;
   const T* V = static_cast<const T*>(a.V) + u.b * a.v.b + u.hk * a.v.h + u.key * a.v.l;
-  const RowFrags<T, DP, held<T, DP>()> kf(K, valid, a.d, grp), vf(WITH_K ? V : K, valid, a.d, grp);
+  RowFrags<T, DP, held<T, DP>()> kf, vf;
+  kf.load(K, valid, a.d, grp);
+  if constexpr (WITH_K) vf.load(V, valid, a.d, grp);
+  kf.arrive();
+  if constexpr (WITH_K) vf.arrive();
   f32x16 dk[WITH_K ? DT : 1], dv[WITH_V ? DT : 1];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -628,7 +689,7 @@ __device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) 
   };
   if constexpr (WITH_K) put(dk, a.dK, a.gk, a.sm_scale, 0);
   if constexpr (WITH_V) put(dv, a.dV, a.gv, 1.f, 1);
- });
+ }
 }
 
 template <typename T, int DP>
@@ -659,14 +720,15 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_dkv_combine_kernel(CrossArgs,
 // ---- host ----
 static int padded_d(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// Forward and dQ.  Two workgroups a CU.
+// Forward and dQ: two workgroups a CU where registers and LDS allow it.
 static Deal rows_deal(const CrossArgs& a) {
   Deal d{};
   d.tile = a.dtype == BSA_BF16 && a.d <= 128 ? 64 : 32;  // key_tile
   d.rows = (int64_t)a.Hkv * ((a.M + kUnitRows - 1) / kUnitRows);
   const int64_t units = d.rows * a.B, tiles = (a.S + d.tile - 1) / d.tile;
-  d.shares = units < 2 * 512 && tiles > 4;
-  d.grid = (int)(d.shares ? std::max<int64_t>(units, std::min<int64_t>(512, units * tiles / 4)) : units);
+  const int slots = a.d <= 64 || (a.dtype == BSA_BF16 && a.d <= 128) ? 512 : 256;
+  d.way = units < 2 * slots && tiles > 4 ? SHARES : EACH;
+  d.grid = (int)(d.way == SHARES ? std::max<int64_t>(units, std::min<int64_t>(slots, units * tiles / 4)) : units);
   return d;
 }
 
@@ -677,12 +739,12 @@ static Deal keys_deal(const CrossArgs& a) {
   d.steps = a.G * query_tiles(a.Lq);
   d.rows = (int64_t)a.Hkv * ((a.S + kUnitRows - 1) / kUnitRows);
   const int64_t units = d.rows * a.B;
-  d.shares = 1;
+  d.way = SHARES;
   d.grid = (int)std::min<int64_t>(256, std::max<int64_t>(units, units * d.steps / 4));
   return d;
 }
 
-static size_t part_bytes(const Deal& d, int values) { return d.shares ? (size_t)2 * d.grid * kWaves * values * 64 * sizeof(float) : 0; }
+static size_t part_bytes(const Deal& d, int values) { return d.way == SHARES ? (size_t)2 * d.grid * kWaves * values * 64 * sizeof(float) : 0; }
 
 size_t cross_fwd_workspace(const CrossArgs& a) { return part_bytes(rows_deal(a), padded_d(a.d) / 2 + 2); }
 
@@ -702,11 +764,13 @@ template <typename T, int DP>
 static int fwd_t(const CrossArgs& a, hipStream_t st) {
   const Deal d = rows_deal(a);
   constexpr size_t lds = 4 * key_tile<T, DP>() * DP * sizeof(T);
-  if (const int rc = allow_dynamic_lds<cross_fwd_kernel<T, DP>>(lds)) return rc;
+  const bool one = d.way == EACH;
+  if (const int rc = one ? allow_dynamic_lds<cross_fwd_kernel<T, DP, true>>(lds) : allow_dynamic_lds<cross_fwd_kernel<T, DP, false>>(lds)) return rc;
   float* part = static_cast<float*>(a.ws);
-  hipLaunchKernelGGL((cross_fwd_kernel<T, DP>), dim3(d.grid), dim3(kThreads), lds, st, a, d, part);
+  if (one) hipLaunchKernelGGL((cross_fwd_kernel<T, DP, true>), dim3(d.grid), dim3(kThreads), lds, st, a, d, part);
+  else hipLaunchKernelGGL((cross_fwd_kernel<T, DP, false>), dim3(d.grid), dim3(kThreads), lds, st, a, d, part);
   if (const int rc = check_launch()) return rc;
-  if (d.shares) hipLaunchKernelGGL((cross_fwd_combine_kernel<T, DP>), dim3((unsigned)(d.rows * a.B), kWaves), dim3(2 * DP), 0, st, a, d, part);
+  if (d.way == SHARES) hipLaunchKernelGGL((cross_fwd_combine_kernel<T, DP>), dim3((unsigned)(d.rows * a.B), kWaves), dim3(2 * DP), 0, st, a, d, part);
   return check_launch();
 }
 
@@ -714,14 +778,16 @@ template <typename T, int DP>
 static int bwd_t(const CrossArgs& a, hipStream_t st) {
   const Deal d = rows_deal(a), k = keys_deal(a);
   constexpr size_t lds = 4 * key_tile<T, DP>() * DP * sizeof(T), klds = 2 * (64 * DP * sizeof(T) + 256);
-  if (const int rc = allow_dynamic_lds<cross_dq_kernel<T, DP>>(lds)) return rc;
+  const bool one = d.way == EACH;
+  if (const int rc = one ? allow_dynamic_lds<cross_dq_kernel<T, DP, true>>(lds) : allow_dynamic_lds<cross_dq_kernel<T, DP, false>>(lds)) return rc;
   const bool fast = fast_dkv(a) && a.near;
   if (const int rc = fast ? grant_cross_dkv_fast(a) : allow_dynamic_lds<cross_dkv_kernel<T, DP>>(klds)) return rc;
   float* stat = static_cast<float*>(a.ws);
   float* part = stat + stat_bytes(a) / sizeof(float);
-  hipLaunchKernelGGL((cross_dq_kernel<T, DP>), dim3(d.grid), dim3(kThreads), lds, st, a, d, stat, part);
+  if (one) hipLaunchKernelGGL((cross_dq_kernel<T, DP, true>), dim3(d.grid), dim3(kThreads), lds, st, a, d, stat, part);
+  else hipLaunchKernelGGL((cross_dq_kernel<T, DP, false>), dim3(d.grid), dim3(kThreads), lds, st, a, d, stat, part);
   if (const int rc = check_launch()) return rc;
-  if (d.shares) hipLaunchKernelGGL((cross_dq_combine_kernel<T, DP>), dim3((unsigned)(d.rows * a.B), kWaves), dim3(2 * DP), 0, st, a, d, part);
+  if (d.way == SHARES) hipLaunchKernelGGL((cross_dq_combine_kernel<T, DP>), dim3((unsigned)(d.rows * a.B), kWaves), dim3(2 * DP), 0, st, a, d, part);
   if (const int rc = check_launch()) return rc;
   if (fast) return launch_cross_dkv_fast(a, stat, part, st);
   hipLaunchKernelGGL((cross_dkv_kernel<T, DP>), dim3(k.grid, DP > 128 ? 2 : 1), dim3(kThreads), klds, st, a, k, stat, part);

@@ -45,7 +45,9 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_fast_kernel(CrossArgs, Deal 
   extern __shared__ __align__(16) uint8_t smem[];  // [4 wavefronts][2 tiles]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  for_pieces(*kernel_args(), dl, threadIdx.x & 63, [&](const Piece& pc) {
+  Dealer<false> dealer(*kernel_args(), dl, threadIdx.x & 63);
+  Piece pc;
+  while (dealer.next(pc)) {
     Args& a = *afresh(kernel_args());
     const int lane = afresh(threadIdx.x & 63), grp = lane >> 5, col = lane & 31;
     const int tile = (int)(pc.unit / a.Hkv), hk = (int)(pc.unit - (int64_t)tile * a.Hkv), b = pc.b, first = tile * kKeys;
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_fast_kernel(CrossArgs, Deal 
       }
     }
     __syncthreads();  // the ring is free
-  });
+  }
 }
 
 // Joins the parts of a unit, and writes the zeros of the units that had no step.  A wavefront has 32 channels of 32 keys.
@@ -366,7 +368,8 @@ __global__ __launch_bounds__(2 * D) void cross_dkv_fast_combine_kernel(CrossArgs
 // One workgroup a CU; a share of sixteen tiles (four a wavefront) at least, or a piece's loads and sums are all that it does.
 static Deal fast_deal(const CrossArgs& a) {
   Deal d{};
-  d.by_keys = d.shares = 1;
+  d.by_keys = 1;
+  d.way = SHARES;
   d.tile = kKeys;
   d.steps = a.G * query_tiles(a.Lq);
   d.rows = (int64_t)a.Hkv * ((a.S + kKeys - 1) / kKeys);
