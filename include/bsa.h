@@ -291,7 +291,7 @@ int bsa_qk_norm_rope_bwd(const bsa_shape_t* shape, const bsa_rope_t* rope, const
  * valid ones, O = softmax(sm_scale Q K^T) V.  Query head h reads key/value head h / (H / Hkv).
  * State s of batch entry b is valid if s < kv_len[b] and kv_mask[b][s] is not 0.  What K and V hold at other states is
  * never used, be it NaN.  A batch entry without a valid state gives O = 0 and LSE = -inf and has no gradients.
- *   shape    1 <= Hkv, Hkv divides H; Lq, S >= 1, (H / Hkv) * Lq < 2^31; d a multiple of 8, at most 256
+ *   shape    1 <= Hkv, Hkv divides H; Lq, S >= 1; B * H * ceil(Lq / 32) * ceil(S / 32) < 2^30; d a multiple of 8, at most 256
  *   q, k, v, o   strides of Q, K, V, O
  *   kv_len   device [B] int32, taken as 0 below 0 and as S above S; NULL: S for all
  *   kv_mask  device [B][S] bytes; NULL: all 1

@@ -352,10 +352,10 @@ static int cross_args(const bsa_cross_shape_t* s, CrossArgs* a) {
   if (s->B <= 0 || s->H <= 0 || s->Hkv <= 0 || s->Lq <= 0 || s->S <= 0 || s->d <= 0) return BSA_ERR_SHAPE;
   if (s->H % s->Hkv || s->d % 8 || s->d > 256) return BSA_ERR_SHAPE;
   const int G = s->H / s->Hkv;
-  if ((int64_t)G * s->Lq > 0x7fffffffLL || s->S > 0x7fffff00) return BSA_ERR_SHAPE;
-  // workgroups of a launch: rows in groups of 32 at least, keys likewise, and the padded row statistics
-  if ((int64_t)s->B * s->H > 0x7fffffffLL) return BSA_ERR_SHAPE;
-  if ((int64_t)s->B * s->H * ((s->Lq + 31) / 32) > 0x3fffffffLL || (int64_t)s->B * s->Hkv * ((s->S + 31) / 32) > 0x3fffffffLL) return BSA_ERR_SHAPE;
+  if ((int64_t)G * s->Lq > 0x7fffff00LL || s->Lq > 0x7fffff00 || s->S > 0x7fffff00) return BSA_ERR_SHAPE;
+  // tiles of 32 queries by 32 keys, heads and batch: the kernels count them in 32 bits
+  const int64_t tiles = (int64_t)((s->Lq + 31) / 32) * ((s->S + 31) / 32), heads = (int64_t)s->B * s->H;
+  if (heads > 0x3fffffffLL / ((s->Lq + 31) / 32 + (s->S + 31) / 32) || tiles > 0x3fffffffLL / heads) return BSA_ERR_SHAPE;
   a->B = s->B; a->H = s->H; a->Hkv = s->Hkv; a->G = G; a->Lq = s->Lq; a->M = G * s->Lq; a->S = s->S; a->d = s->d; a->dtype = s->dtype;
   return BSA_OK;
 }

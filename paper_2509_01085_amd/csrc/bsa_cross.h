@@ -277,16 +277,15 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 // 512 keys, forward 151 and 159 us.)
 enum { EACH = 0, SHARES = 1 };
 struct Deal {
-  int grid;      // workgroups
+  int grid;     // workgroups
   int way;
-  int by_keys;   // units are tiles of `tile` keys and take `steps` steps; else `rows` units an entry of a step per `tile` valid keys
+  int by_keys;  // units are tiles of `tile` keys and take `steps` steps; else `rows` units an entry of a step per `tile` valid keys
   int tile, steps;
-  int64_t rows;  // units of a batch entry: (by_keys) of S keys
-};
+  int rows;     // units of a batch entry: (by_keys) of S keys
+};  // (all steps of a launch together: less than 2^31, the host has made sure)
 
-// A value that is the same in all lanes, in scalar registers.
+// A value that is the same in all lanes, in a scalar register.
 __device__ inline int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ inline int64_t same(int64_t v) { return (int64_t)uniform64((const void*)v); }
 
 struct Ledger {
   const Deal& dl;
@@ -294,40 +293,47 @@ struct Ledger {
   int B, S, Hkv, lane;
   __device__ inline Ledger(Args& a, const Deal& dl_, int lane_) : dl(dl_), len(a.kv_len), B(a.B), S(a.S), Hkv(a.Hkv), lane(lane_) {}
   __device__ inline int valid(int b) const { return len ? max(0, min(len[b], S)) : S; }  // b may differ from lane to lane
-  __device__ inline int tiles(int b) const { return (valid(b) + dl.tile - 1) / dl.tile; }
+  __device__ inline int tiles(int b) const { return (int)((uint32_t)(valid(b) + dl.tile - 1) / (uint32_t)dl.tile); }
   __device__ inline int steps(int b) const { return dl.by_keys ? dl.steps : tiles(b); }
-  __device__ inline int64_t units(int b) const { return dl.by_keys ? (int64_t)Hkv * tiles(b) : dl.rows; }  // that take steps
-  __device__ inline int64_t weight(int b) const { return units(b) * steps(b); }
-  __device__ inline int64_t scan(int64_t v) const {  // inclusive, over the lanes
+  __device__ inline int units(int b) const { return dl.by_keys ? Hkv * tiles(b) : dl.rows; }  // that take steps
+  __device__ inline int weight(int b) const { return units(b) * steps(b); }
+  __device__ inline int scan(int v) const {  // inclusive, over the lanes
     const int lane = afresh(this->lane);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const int64_t w = __shfl_up(v, o);
+      const int w = __shfl_up(v, o);
       if (lane >= o) v += w;
     }
     return v;
   }
-  // Steps of the entries below b (of all with b = B).
-  __device__ inline int64_t below(int b) const {
-    if (!len) return b * weight(0);
-    int64_t sum = 0;
-    for (int b0 = 0; b0 < b; b0 += 64) sum += same(__shfl(scan(b0 + lane < b ? weight(b0 + lane) : 0), 63));
+  // Steps of all entries; `below`: of those below b.
+  __device__ inline int total(int b, int& below) const {
+    if (!len) {
+      const int w = weight(0);
+      below = b * w;
+      return B * w;
+    }
+    int sum = 0;
+    for (int b0 = 0; b0 < B; b0 += 64) {
+      const int v = b0 + lane < B ? weight(b0 + lane) : 0, to = scan(v);
+      if (b >= b0 && b < b0 + 64) below = sum + same(__shfl(to - v, b - b0));
+      sum += same(__shfl(to, 63));
+    }
     return sum;
   }
-  // The entry that `pos` is of, and where it begins.
-  __device__ inline int entry(int64_t pos, int64_t& base) const {
+  // The entry that step `pos` is of, and the step that it begins with.
+  __device__ inline int entry(int pos, int& base) const {
     if (!len) {
-      const int64_t w = weight(0);
-      const int b = (int)(pos / w);
+      const int w = weight(0), b = (int)((uint32_t)pos / (uint32_t)w);
       base = b * w;
       return b;
     }
     base = 0;
     for (int b0 = 0;; b0 += 64) {
-      const int64_t v = b0 + lane < B ? weight(b0 + lane) : 0, to = scan(v);
+      const int v = b0 + lane < B ? weight(b0 + lane) : 0, to = scan(v);
       const uint64_t past = __ballot(base + to > pos);
       if (past || b0 + 64 >= B) {
-        const int l = __builtin_amdgcn_readfirstlane(__builtin_ctzll(past | (1ull << 63)));
+        const int l = same(__builtin_ctzll(past | (1ull << 63)));
         base += same(__shfl(to - v, l));
         return b0 + l;
       }
@@ -339,34 +345,34 @@ struct Ledger {
 // One piece of a workgroup's work: steps t0 .. t1 - 1 of a unit.
 struct Piece {
   int b, t0, t1;
-  int64_t unit;   // of the entry
-  int slot;       // of its partial results; -1: the unit is whole
+  int unit;   // of the entry
+  int slot;   // of its partial results; -1: the unit is whole
 };
 
 // A workgroup's pieces, one after the other.  ONE: EACH, so there is one.
 template <bool ONE>
 struct Dealer {
   const Ledger led;
-  int64_t pos, end, units, unit;
-  int b, t, steps;
+  int pos, end, units, unit, b, t, steps;
   bool fresh;  // no piece taken yet
   __device__ inline Dealer(Args& a, const Deal& dl, int lane) : led(a, dl, lane), t(0), fresh(true) {
     if constexpr (ONE) {
-      b = dl.rows == 1 ? blockIdx.x : blockIdx.x / (uint32_t)dl.rows;  // (units of a launch: less than 2^31)
-      unit = blockIdx.x - (uint32_t)b * (uint32_t)dl.rows;
+      b = (int)(blockIdx.x / (uint32_t)dl.rows);
+      unit = (int)blockIdx.x - b * dl.rows;
       steps = same(led.steps(b));
       return;
     }
-    const int64_t total = led.below(a.B), per = (total + dl.grid - 1) / dl.grid;
-    pos = blockIdx.x * per;
+    int none = 0;
+    const int total = led.total(-1, none), per = (int)((uint32_t)(total + dl.grid - 1) / (uint32_t)dl.grid);
+    pos = min((int)blockIdx.x * per, total);  // (grid * per < total + grid)
     end = min(pos + per, total);
     if (pos >= end) return;
-    const int64_t base = enter();
-    unit = (pos - base) / steps;
-    t = (int)(pos - base - unit * steps);
+    const int base = enter();
+    unit = (int)((uint32_t)(pos - base) / (uint32_t)steps);
+    t = pos - base - unit * steps;
   }
-  __device__ inline int64_t enter() {
-    int64_t base;
+  __device__ inline int enter() {
+    int base;
     b = led.entry(pos, base);
     steps = same(led.steps(b));
     units = same(led.units(b));
@@ -383,7 +389,7 @@ struct Dealer {
     pc.b = b;
     pc.unit = unit;
     pc.t0 = t;
-    pc.t1 = (int)min((int64_t)steps, t + (end - pos));
+    pc.t1 = min(steps, t + (end - pos));
     pc.slot = t == 0 && pc.t1 == steps ? -1 : 2 * (int)blockIdx.x + !fresh;
     pos += pc.t1 - t;
     t = 0;  // (a share ends in a unit's middle or goes on with the next unit)
@@ -395,26 +401,26 @@ struct Dealer {
 
 // The partial results of a unit of entry b: how many there are (0: the unit is whole, -1: nobody worked on it) and their slots.
 struct Parts {
-  int n;
-  int64_t per, first, w0;
-  __device__ inline Parts(Args& a, const Deal& dl, int lane, int b, int64_t unit) : n(-1), per(0), first(0), w0(0) {
+  int n, per, first, w0;
+  __device__ inline Parts(Args& a, const Deal& dl, int lane, int b, int unit) : n(-1), per(0), first(0), w0(0) {
     const Ledger led(a, dl, lane);
-    const int steps = led.steps(b);
-    if (dl.way != SHARES || steps == 0 || unit >= led.units(b)) return;
-    const int64_t total = led.below(a.B);
-    per = (total + dl.grid - 1) / dl.grid;
-    first = led.below(b) + unit * steps;
-    w0 = first / per;
-    n = (int)((first + steps - 1) / per - w0);
+    const int steps = same(led.steps(b));
+    if (dl.way != SHARES || steps == 0 || unit >= same(led.units(b))) return;
+    int below = 0;
+    const int total = led.total(b, below);
+    per = (int)((uint32_t)(total + dl.grid - 1) / (uint32_t)dl.grid);
+    first = below + unit * steps;
+    w0 = (int)((uint32_t)first / (uint32_t)per);
+    n = (int)((uint32_t)(first + steps - 1) / (uint32_t)per) - w0;
     if (n) ++n;
   }
-  __device__ inline int64_t slot(int k) const { return 2 * (w0 + k) + ((w0 + k) * per < first); }
+  __device__ inline int slot(int k) const { return 2 * (w0 + k) + ((w0 + k) * per < first); }
 };
 
 // Partial results: [slot][wavefront][value][lane] floats.
 template <int VALUES>
-__device__ inline float* part_of(float* base, int64_t slot, int wave, int lane) {
-  return base + ((slot * kWaves + wave) * VALUES) * 64 + lane;
+__device__ inline float* part_of(float* base, int slot, int wave, int lane) {
+  return base + (((int64_t)slot * kWaves + wave) * VALUES) * 64 + lane;
 }
 
 // The query tiles of dK and dV: 32 tokens of a head from first_token(i) on; where the last one would reach past Lq it begins

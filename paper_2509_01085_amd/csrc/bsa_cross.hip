@@ -17,14 +17,14 @@ template <typename T, int DP> constexpr int key_tile() { return sizeof(T) == 2 &
 struct RowUnit {
   int b, hk, m, g, l;  // batch entry, key head, row, its head in the group and token
   bool live, any;      // this row, any of the wavefront's exists
-  __device__ inline RowUnit(Args& a, int b_, int64_t unit /* of the entry */, int wave, int lane) : b(b_) {
+  __device__ inline RowUnit(Args& a, int b_, int unit /* of the entry */, int wave, int lane) : b(b_) {
     const int of_head = (a.M + kUnitRows - 1) / kUnitRows;
-    hk = (int)(unit / of_head);
-    const int first = (int)(unit - (int64_t)hk * of_head) * kUnitRows + 32 * wave;
+    hk = (int)((uint32_t)unit / (uint32_t)of_head);
+    const int first = (unit - hk * of_head) * kUnitRows + 32 * wave;
     any = first < a.M;
     m = first + (lane & 31);
     live = m < a.M;
-    g = live ? m / a.Lq : 0;
+    g = live && a.G > 1 ? (int)((uint32_t)m / (uint32_t)a.Lq) : 0;
     l = live ? m - g * a.Lq : 0;
   }
   __device__ inline int head(Args& a) const { return hk * a.G + g; }
@@ -32,7 +32,7 @@ struct RowUnit {
   __device__ inline int64_t flat(Args& a) const { return ((int64_t)b * a.H + head(a)) * a.Lq + l; }
 };
 
-__device__ inline int key_head(Args& a, int64_t unit) { return (int)(unit / ((a.M + kUnitRows - 1) / kUnitRows)); }
+__device__ inline int key_head(Args& a, int unit) { return (int)((uint32_t)unit / (uint32_t)((a.M + kUnitRows - 1) / kUnitRows)); }
 
 // Chunk c of a row, zeros where there is none.
 template <typename T>
@@ -89,7 +89,7 @@ struct RowFrags {
     return sum;
   }
 };
-template <typename T, int DP> constexpr int two_a_cu() { return sizeof(T) == 2 && DP <= 128 ? 2 : 1; }
+template <typename T, int DP> constexpr int two_a_cu() { return DP <= 128 ? 2 : 1; }
 template <typename T, int DP> constexpr bool held() { return DP <= 128; }
 
 // ---- forward ----
@@ -344,26 +344,27 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_fwd_kerne
 }
 
 // Sum over the parts of a unit of the 16 values that a wavefront's channel tile has at `at` (values before it), each part times its
-// weight: four parts' loads in flight.
+// weight: eight parts' loads in flight.
 template <int VALUES, typename F>
 __device__ inline f32x16 sum_parts(float* part, const Parts& ps, int at, int wave, int lane, F weight) {
   f32x16 acc;
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-  for (int s = 0; s < ps.n; s += 4) {
-    float v[4][16], f[4];
+  for (int s = 0; s < ps.n; s += 8) {
+    float v[8][16], f[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 8; ++j) {
       const float* in = part_of<VALUES>(part, ps.slot(min(s + j, ps.n - 1)), wave, lane) + at * 64;
 #pragma unroll
       for (int r = 0; r < 16; ++r) v[j][r] = in[r * 64];
-      f[j] = weight(min(s + j, ps.n - 1));
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (s + j < ps.n && f[j] != 0.f)  // (a part without a valid key holds nothing)
+    for (int j = 0; j < 8; ++j) f[j] = weight(min(s + j, ps.n - 1));
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] = __builtin_fmaf(v[j][r], f[j], acc[r]);
+    for (int j = 0; j < 8; ++j)
+      if (s + j < ps.n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = f[j] != 0.f ? __builtin_fmaf(v[j][r], f[j], acc[r]) : acc[r];  // (a part without a key holds nothing)
   }
   return acc;
 }
@@ -375,8 +376,7 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_fwd_combine_kernel(CrossArgs,
   Args& a = *kernel_args();
   constexpr int DT = DP / 32, VALUES = DT * 16 + 2;
   const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.y, grp = lane >> 5;
-  const int b = (int)(blockIdx.x / dl.rows);
-  const int64_t unit = blockIdx.x - b * dl.rows;
+  const int b = (int)(blockIdx.x / (uint32_t)dl.rows), unit = (int)blockIdx.x - b * dl.rows;
   const RowUnit u(a, b, unit, wave, lane);
   if (!u.any) return;
   const Parts ps(a, dl, lane, b, unit);
@@ -385,20 +385,33 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_fwd_combine_kernel(CrossArgs,
   auto sum_of = [&](int s) { return part_of<VALUES>(part, ps.slot(s), wave, lane)[(DT * 16 + 1) * 64]; };
   float m = kLowest, l = 0.f;
   bool any = false;
-#pragma unroll 4
-  for (int s = 0; s < ps.n; ++s) {
-    const float ms = top_of(s), ls = sum_of(s);
-    any |= ls != -1.f;
-    m = fmaxf(m, ls == -1.f ? kLowest : ms);
+  for (int s = 0; s < ps.n; s += 8) {
+    float ms[8], ls[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      ms[j] = top_of(min(s + j, ps.n - 1));
+      ls[j] = sum_of(min(s + j, ps.n - 1));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {  // (the last part again and again changes nothing: sums are taken below)
+      any |= ls[j] != -1.f;
+      m = fmaxf(m, ls[j] == -1.f ? kLowest : ms[j]);
+    }
   }
   auto weight = [&](int s) {
     const float ms = top_of(s), ls = sum_of(s);
     return ls == -1.f ? 0.f : __builtin_amdgcn_exp2f(ms - m);
   };
-#pragma unroll 4
-  for (int s = 0; s < ps.n; ++s) {
-    const float ls = sum_of(s);
-    l = __builtin_fmaf(ls == -1.f ? 0.f : ls, weight(s), l);
+  for (int s = 0; s < ps.n; s += 8) {
+    float ms[8], ls[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      ms[j] = top_of(min(s + j, ps.n - 1));
+      ls[j] = sum_of(min(s + j, ps.n - 1));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (s + j < ps.n && ls[j] != -1.f) l = __builtin_fmaf(ls[j], __builtin_amdgcn_exp2f(ms[j] - m), l);
   }
   const f32x16 o[1] = {sum_parts<VALUES>(part, ps, dt * 16, wave, lane, weight)};
   store_column<T, 1>(static_cast<T*>(a.O_out) + u.offset(a, a.o) + 32 * dt, o, any ? 1.f / l : 0.f, a.d - 32 * dt, grp, u.live);
@@ -491,7 +504,7 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel
     const float c = a.sm_scale * kLog2e;
     const RowUnit u(a, pc.b, pc.unit, wave, lane);
     RowFrags<T, DP, held<T, DP>()> q;
-    RowFrags<T, DP, held<T, DP>()> gr;
+    RowFrags<T, DP, held<T, DP>() && DP * sizeof(T) <= 256> gr;  // (fp32, 128 channels: Q, dQ and this are more than two workgroups' share)
     q.load(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
     gr.load(static_cast<const T*>(a.dO) + u.offset(a, a.go), u.live, a.d, grp);
     const float delta = pair_sum(gr.dot(static_cast<const T*>(a.O) + u.offset(a, a.o)));
@@ -555,8 +568,7 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_dq_combine_kernel(CrossArgs, 
   Args& a = *kernel_args();
   constexpr int DT = DP / 32;
   const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.y;
-  const int b = (int)(blockIdx.x / dl.rows);
-  const int64_t unit = blockIdx.x - b * dl.rows;
+  const int b = (int)(blockIdx.x / (uint32_t)dl.rows), unit = (int)blockIdx.x - b * dl.rows;
   const RowUnit u(a, b, unit, wave, lane);
   if (!u.any) return;
   const Parts ps(a, dl, lane, b, unit);
@@ -571,9 +583,9 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_dq_combine_kernel(CrossArgs, 
 struct KeyUnit {
   int b, hk, first, key;
   bool there;   // the lane's key exists
-  __device__ inline KeyUnit(Args& a, int b_, int64_t unit, int wave, int lane) : b(b_) {
-    const int tile = (int)(unit / a.Hkv);
-    hk = (int)(unit - (int64_t)tile * a.Hkv);
+  __device__ inline KeyUnit(Args& a, int b_, int unit, int wave, int lane) : b(b_) {
+    const int tile = (int)((uint32_t)unit / (uint32_t)a.Hkv);
+    hk = unit - tile * a.Hkv;
     first = tile * kUnitRows;
     key = first + 32 * wave + (lane & 31);
     there = key < a.S;
@@ -706,8 +718,7 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_dkv_combine_kernel(CrossArgs,
   constexpr int DT = DP / 32;
   const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.y;
   const bool is_v = blockIdx.z;
-  const int b = (int)(blockIdx.x / dl.rows);
-  const int64_t unit = blockIdx.x - b * dl.rows;
+  const int b = (int)(blockIdx.x / (uint32_t)dl.rows), unit = (int)blockIdx.x - b * dl.rows;
   const KeyUnit u(a, b, unit, wave, lane);
   const Parts ps(a, dl, lane, b, unit);
   if (ps.n == 0) return;
@@ -720,15 +731,18 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_dkv_combine_kernel(CrossArgs,
 // ---- host ----
 static int padded_d(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// Forward and dQ: two workgroups a CU where registers and LDS allow it.
+// Forward and dQ: two workgroups a CU where registers and LDS allow it.  Shares where whole units would leave workgroups without work for
+// the time of kWorth tiles: what shares cost, the reckoning and the second launch, is about 14 us, a tile 1.2.
+constexpr int kWorth = 12;
 static Deal rows_deal(const CrossArgs& a) {
   Deal d{};
   d.tile = a.dtype == BSA_BF16 && a.d <= 128 ? 64 : 32;  // key_tile
-  d.rows = (int64_t)a.Hkv * ((a.M + kUnitRows - 1) / kUnitRows);
-  const int64_t units = d.rows * a.B, tiles = (a.S + d.tile - 1) / d.tile;
-  const int slots = a.d <= 64 || (a.dtype == BSA_BF16 && a.d <= 128) ? 512 : 256;
-  d.way = units < 2 * slots && tiles > 4 ? SHARES : EACH;
-  d.grid = (int)(d.way == SHARES ? std::max<int64_t>(units, std::min<int64_t>(slots, units * tiles / 4)) : units);
+  d.rows = a.Hkv * ((a.M + kUnitRows - 1) / kUnitRows);
+  const int64_t units = (int64_t)d.rows * a.B, tiles = (a.S + d.tile - 1) / d.tile;
+  const int slots = a.d <= 128 ? 512 : 256;
+  const int64_t idle = ((units + slots - 1) / slots * slots - units) * tiles;  // of all slots together
+  d.way = units < 2 * slots && idle > (int64_t)kWorth * slots ? SHARES : EACH;
+  d.grid = (int)(d.way == SHARES ? std::min<int64_t>(slots, std::max<int64_t>(1, units * tiles / 4)) : units);
   return d;
 }
 
@@ -737,8 +751,8 @@ static Deal keys_deal(const CrossArgs& a) {
   d.by_keys = 1;
   d.tile = kUnitRows;
   d.steps = a.G * query_tiles(a.Lq);
-  d.rows = (int64_t)a.Hkv * ((a.S + kUnitRows - 1) / kUnitRows);
-  const int64_t units = d.rows * a.B;
+  d.rows = a.Hkv * ((a.S + kUnitRows - 1) / kUnitRows);
+  const int64_t units = (int64_t)d.rows * a.B;
   d.way = SHARES;
   d.grid = (int)std::min<int64_t>(256, std::max<int64_t>(units, units * d.steps / 4));
   return d;
@@ -770,7 +784,7 @@ static int fwd_t(const CrossArgs& a, hipStream_t st) {
   if (one) hipLaunchKernelGGL((cross_fwd_kernel<T, DP, true>), dim3(d.grid), dim3(kThreads), lds, st, a, d, part);
   else hipLaunchKernelGGL((cross_fwd_kernel<T, DP, false>), dim3(d.grid), dim3(kThreads), lds, st, a, d, part);
   if (const int rc = check_launch()) return rc;
-  if (d.way == SHARES) hipLaunchKernelGGL((cross_fwd_combine_kernel<T, DP>), dim3((unsigned)(d.rows * a.B), kWaves), dim3(2 * DP), 0, st, a, d, part);
+  if (d.way == SHARES) hipLaunchKernelGGL((cross_fwd_combine_kernel<T, DP>), dim3((unsigned)d.rows * a.B, kWaves), dim3(2 * DP), 0, st, a, d, part);
   return check_launch();
 }
 
@@ -787,12 +801,12 @@ static int bwd_t(const CrossArgs& a, hipStream_t st) {
   if (one) hipLaunchKernelGGL((cross_dq_kernel<T, DP, true>), dim3(d.grid), dim3(kThreads), lds, st, a, d, stat, part);
   else hipLaunchKernelGGL((cross_dq_kernel<T, DP, false>), dim3(d.grid), dim3(kThreads), lds, st, a, d, stat, part);
   if (const int rc = check_launch()) return rc;
-  if (d.way == SHARES) hipLaunchKernelGGL((cross_dq_combine_kernel<T, DP>), dim3((unsigned)(d.rows * a.B), kWaves), dim3(2 * DP), 0, st, a, d, part);
+  if (d.way == SHARES) hipLaunchKernelGGL((cross_dq_combine_kernel<T, DP>), dim3((unsigned)d.rows * a.B, kWaves), dim3(2 * DP), 0, st, a, d, part);
   if (const int rc = check_launch()) return rc;
   if (fast) return launch_cross_dkv_fast(a, stat, part, st);
   hipLaunchKernelGGL((cross_dkv_kernel<T, DP>), dim3(k.grid, DP > 128 ? 2 : 1), dim3(kThreads), klds, st, a, k, stat, part);
   if (const int rc = check_launch()) return rc;
-  hipLaunchKernelGGL((cross_dkv_combine_kernel<T, DP>), dim3((unsigned)(k.rows * a.B), kWaves, 2), dim3(2 * DP), 0, st, a, k, part);
+  hipLaunchKernelGGL((cross_dkv_combine_kernel<T, DP>), dim3((unsigned)k.rows * a.B, kWaves, 2), dim3(2 * DP), 0, st, a, k, part);
   return check_launch();
 }
 

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_fast_kernel(CrossArgs, Deal 
   while (dealer.next(pc)) {
     Args& a = *afresh(kernel_args());
     const int lane = afresh(threadIdx.x & 63), grp = lane >> 5, col = lane & 31;
-    const int tile = (int)(pc.unit / a.Hkv), hk = (int)(pc.unit - (int64_t)tile * a.Hkv), b = pc.b, first = tile * kKeys;
+    const int tile = (int)((uint32_t)pc.unit / (uint32_t)a.Hkv), hk = pc.unit - tile * a.Hkv, b = pc.b, first = tile * kKeys;
     const Keys keys(a, b);
     const uint64_t valid = keys.bits(first, kKeys, lane);
     const int items = valid ? pc.t1 - pc.t0 : 0;
@@ -334,28 +334,27 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_fast_kernel(CrossArgs, Deal 
 
 // Joins the parts of a unit, and writes the zeros of the units that had no step.  A wavefront has 32 channels of 32 keys.
 template <int D>
-__global__ __launch_bounds__(2 * D) void cross_dkv_fast_combine_kernel(CrossArgs, Deal dl, const float* part) {
+__global__ __launch_bounds__(2 * D, 1) void cross_dkv_fast_combine_kernel(CrossArgs, Deal dl, const float* part) {
   Args& a = *kernel_args();
   constexpr int DT = D / 32, NT = 2 * DT;
   const int lane = threadIdx.x & 63, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y, pass = blockIdx.z;
-  const int b = (int)(blockIdx.x / dl.rows);
-  const int64_t unit = blockIdx.x - b * dl.rows;
+  const int b = (int)(blockIdx.x / (uint32_t)dl.rows), unit = (int)blockIdx.x - b * dl.rows;
   const Parts ps(a, dl, lane, b, unit);
   if (ps.n == 0) return;
-  const int tile = (int)(unit / a.Hkv), hk = (int)(unit - (int64_t)tile * a.Hkv), key = tile * kKeys + 32 * h + (lane & 31);
+  const int tile = (int)((uint32_t)unit / (uint32_t)a.Hkv), hk = unit - tile * a.Hkv, key = tile * kKeys + 32 * h + (lane & 31);
   f32x16 acc[1];
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[0][r] = 0.f;
-  for (int s = 0; s < ps.n; s += 4) {
-    float v[4][16];
+  for (int s = 0; s < ps.n; s += 8) {
+    float v[8][16];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float* in = part + ((ps.slot(min(s + j, ps.n - 1)) * 2 + pass) * NT + h * DT + dt) * 1024 + lane;
+    for (int j = 0; j < 8; ++j) {
+      const float* in = part + (((int64_t)ps.slot(min(s + j, ps.n - 1)) * 2 + pass) * NT + h * DT + dt) * 1024 + lane;
 #pragma unroll
       for (int r = 0; r < 16; ++r) v[j][r] = in[r * 64];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 8; ++j)
       if (s + j < ps.n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[0][r] += v[j][r];
@@ -372,8 +371,8 @@ static Deal fast_deal(const CrossArgs& a) {
   d.way = SHARES;
   d.tile = kKeys;
   d.steps = a.G * query_tiles(a.Lq);
-  d.rows = (int64_t)a.Hkv * ((a.S + kKeys - 1) / kKeys);
-  d.grid = (int)std::min<int64_t>(256, std::max<int64_t>(1, d.rows * a.B * d.steps / 16));
+  d.rows = a.Hkv * ((a.S + kKeys - 1) / kKeys);
+  d.grid = (int)std::min<int64_t>(256, std::max<int64_t>(1, (int64_t)d.rows * a.B * d.steps / 16));
   return d;
 }
 
@@ -387,7 +386,7 @@ static int launch_t(const CrossArgs& a, const float* stat, float* part, hipStrea
   if (a.d == D) hipLaunchKernelGGL((cross_dkv_fast_kernel<D, true>), dim3(d.grid), dim3(256), lds_bytes<D>(), st, a, d, stat, part);
   else hipLaunchKernelGGL((cross_dkv_fast_kernel<D, false>), dim3(d.grid), dim3(256), lds_bytes<D>(), st, a, d, stat, part);
   if (const int rc = check_launch()) return rc;
-  hipLaunchKernelGGL((cross_dkv_fast_combine_kernel<D>), dim3((unsigned)(d.rows * a.B), 2, 2), dim3(2 * D), 0, st, a, d, part);
+  hipLaunchKernelGGL((cross_dkv_fast_combine_kernel<D>), dim3((unsigned)d.rows * a.B, 2, 2), dim3(2 * D), 0, st, a, d, part);
   return check_launch();
 }
 
