@@ -312,7 +312,8 @@ int bsa_cross_attn_fwd(const bsa_cross_shape_t* shape, const void* Q, const void
 
 /*
  * Its backward.  dK and dV are sums over the query heads that share them, zero at states that are not valid; every
- * element of dQ, dK and dV is written.  delta = <dO, O> uses the O the caller passes.
+ * element of dQ, dK and dV is written.  delta = <dO, O> uses the O the caller passes (bf16, d <= 128: batch entries with
+ * at most 128 states have it from the probabilities instead, the same number without the rounding of O).
  *   O, LSE   the forward's outputs
  *   grads    host, strides of dO, dQ, dK, dV, in this order; NULL: those of O, Q, K, V
  *   K and V that repeat (stride 0) have a gradient for every repetition, whose sum is the caller's.
