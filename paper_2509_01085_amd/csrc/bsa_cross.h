@@ -32,6 +32,9 @@ __device__ inline int afresh(int lane) {
   return lane;
 }
 
+// A value that is the same in all lanes, in a scalar register.
+__device__ inline int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // ---- element types ----
 template <typename T> struct Elt;
 template <> struct Elt<uint16_t> {
@@ -161,35 +164,42 @@ struct Requests {
   using V = TileView<T, DP>;
   static constexpr int N = ROWS * V::CPR / NT;  // requests of a thread
   static_assert(ROWS * V::CPR % NT == 0, "whole requests");
-  // Where an instruction's rows are a multiple of 16, the swizzle is the same for all and they differ by a scalar step.
+  // The rows of the next instruction are a scalar step on, and where they are 16 or a multiple, the swizzle is the same.
   static constexpr bool STEPS = NT / V::CPR % 16 == 0;
-  uint32_t off[STEPS ? 1 : N];  // byte offsets from the tile's first row; not used unless they fit (near)
+  uint32_t off;  // byte offset from the tile's first row; not used unless all fit (near)
   int64_t step;
   int tid, d;
   __device__ inline int row(int n) const { return (n * NT + tid) / V::CPR; }
   __device__ inline int channel(int n) const { return (((n * NT + tid) % V::CPR) ^ tile_swz<T, DP>(row(n))) * V::E::CE; }
   __device__ inline Requests(int64_t stride, int d_, int tid_) : step(NT / V::CPR * stride * (int64_t)sizeof(T)), tid(tid_), d(d_) {
-#pragma unroll
-    for (int n = 0; n < (STEPS ? 1 : N); ++n) off[n] = (uint32_t)((row(n) * stride + channel(n)) * (int64_t)sizeof(T));
+    off = (uint32_t)((row(0) * stride + channel(0)) * (int64_t)sizeof(T));
   }
-  __device__ inline void clear(uint8_t* tile) const {
+  __device__ __forceinline__ void clear(uint8_t* tile) const {
 #pragma unroll
     for (int n = 0; n < N; ++n)
       if (channel(n) >= d) *reinterpret_cast<u32x4*>(tile + (n * NT + tid) * 16) = u32x4{0, 0, 0, 0};
   }
   // All rows of the tile are there and offsets fit: no arithmetic for a lane.
-  __device__ inline void whole(uint8_t* tile, const T* base) const {
+  __device__ __forceinline__ void whole(uint8_t* tile, const T* base) const {
     const uint64_t sbase = uniform64(base);
     const uint32_t lds = uniform_lds(tile + (tid >> 6) * 1024);
 #pragma unroll
     for (int n = 0; n < N; ++n)
       if (channel(n) < d) {
-        if constexpr (STEPS) dma16_raw(sbase + n * step, off[0], lds + n * NT * 16);
-        else dma16_raw(sbase, off[n], lds + n * NT * 16);
+        const uint64_t from = uniform64((const void*)(sbase + n * step));  // (behind a condition of the lane's, and still the same for all)
+        dma16_raw(from, STEPS ? off : off + (channel(n) - channel(0)) * (int)sizeof(T), same(lds + n * NT * 16));
       }
   }
+  // The first `left` rows are there (offsets fit); the last of them stands in for the others, whose weights are zero.
+  __device__ __forceinline__ void cut(uint8_t* tile, const T* base, int64_t stride, int left) const {
+    const uint64_t sbase = uniform64(base);
+    const uint32_t lds = uniform_lds(tile + (tid >> 6) * 1024), step = (uint32_t)(stride * (int64_t)sizeof(T));
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (channel(n) < d) dma16_raw(uniform64((const void*)sbase), min(row(n), left - 1) * step + channel(n) * (uint32_t)sizeof(T), same(lds + n * NT * 16));
+  }
   // Rows whose bit in `there` is not set arrive as zeros.
-  __device__ inline void some(uint8_t* tile, const T* base, int64_t stride, uint64_t there) const {
+  __device__ __forceinline__ void some(uint8_t* tile, const T* base, int64_t stride, uint64_t there) const {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll 1
     for (int n = 0; n < N; ++n) {
@@ -198,22 +208,24 @@ struct Requests {
       dma16(src, tile + (n * NT + wave * 64) * 16);
     }
   }
-  __device__ inline void operator()(uint8_t* tile, const T* base, int64_t stride, uint64_t there, bool near) const {
+  __device__ __forceinline__ void operator()(uint8_t* tile, const T* base, int64_t stride, uint64_t there, bool near) const {
     if (near && there == (ROWS == 64 ? ~0ull : (1ull << ROWS) - 1)) whole(tile, base);
+    else if (near && there && !(there & (there + 1))) cut(tile, base, stride, __popcll(there));
     else some(tile, base, stride, there);
   }
 };
 
 // Which of the KT keys from `first` on are valid, as bits.
 struct Keys {
-  int n;                 // valid length
+  int n;                 // valid length (b is the same for all lanes: a scalar load)
   const uint8_t* mask;   // the batch entry's, or NULL
-  __device__ inline Keys(Args& a, int b) : n(a.kv_len ? __builtin_amdgcn_readfirstlane(max(0, min(a.kv_len[b], a.S))) : a.S), mask(a.kv_mask ? a.kv_mask + (int64_t)b * a.S : nullptr) {}
+  __device__ inline Keys(Args& a, int b) : n(a.kv_len ? max(0, min(((const __attribute__((address_space(4))) int32_t*)a.kv_len)[b], a.S)) : a.S), mask(a.kv_mask ? a.kv_mask + (int64_t)b * a.S : nullptr) {}
   __device__ inline uint64_t bits(int first, int count, int lane) const {
     if (!mask) {  // (uniform: a length alone)
       const int left = n - first;
       return left >= count ? (count == 64 ? ~0ull : (1ull << count) - 1) : left <= 0 ? 0 : (1ull << left) - 1;
     }
+    // (The load is waited for here.  Asked for a tile ahead, or 64 tiles ahead, it cost every walk more than masks gained by it.)
     const int s = first + lane;
     const bool in = lane < count && s < n;
     const uint8_t m = mask[in ? s : 0];
@@ -283,9 +295,6 @@ struct Deal {
   int tile, steps;
   int rows;     // units of a batch entry: (by_keys) of S keys
 };  // (all steps of a launch together: less than 2^31, the host has made sure)
-
-// A value that is the same in all lanes, in a scalar register.
-__device__ inline int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 struct Ledger {
   const Deal& dl;

@@ -123,9 +123,8 @@ struct KvRing {
   }
   __device__ inline const uint8_t* k_tile(int place) const { return smem + place * 2 * TILE; }
   __device__ inline const uint8_t* v_tile(int place) const { return k_tile(place) + TILE; }
-  // Tile t of key head hk into a place of the ring; returns its valid keys.
-  __device__ inline uint64_t request(Args& a, int b, int hk, int t, int place) const {
-    const uint64_t there = Keys(a, b).bits(t * KT, KT, lane);
+  // Tile t of key head hk, whose valid keys are `there`, into a place of the ring.
+  __device__ __forceinline__ uint64_t request(Args& a, uint64_t there, int b, int hk, int t, int place) const {
     const T* K = static_cast<const T*>(a.K) + b * a.k.b + hk * a.k.h + (int64_t)t * KT * a.k.l;
     const T* V = static_cast<const T*>(a.V) + b * a.v.b + hk * a.v.h + (int64_t)t * KT * a.v.l;
     uint8_t* at = smem + place * 2 * TILE;
@@ -140,6 +139,7 @@ struct KvRing {
 // next one's: `place` is the multiplied tile's, the other one the requested tile's.
 template <typename T, int DP>
 struct Walk {
+  static constexpr int KT = key_tile<T, DP>();
   const KvRing<T, DP>& ring;
   int place = 0;
   bool asked = false;  // the coming piece's first tile has been requested
@@ -148,13 +148,13 @@ struct Walk {
   bool here = false;
   __device__ inline explicit Walk(const KvRing<T, DP>& r) : ring(r) {}
   // Requests a piece's first tile, unless that was done while the piece before it ended.
-  __device__ inline void ask(Args& a, const Piece& pc, int hk) {
-    if (!asked && pc.t0 < pc.t1) bits = ring.request(a, pc.b, hk, pc.t0, place);
+  __device__ __forceinline__ void ask(Args& a, const Piece& pc, int hk) {
+    if (!asked && pc.t0 < pc.t1) bits = ring.request(a, Keys(a, pc.b).bits(pc.t0 * KT, KT, ring.lane), pc.b, hk, pc.t0, place);
     asked = true;
   }
   // Both tiles of a piece of one or two, now.
-  __device__ inline void both(Args& a, const Piece& pc, int hk) {
-    if (pc.t1 == 2) second = ring.request(a, pc.b, hk, 1, place ^ 1);
+  __device__ __forceinline__ void both(Args& a, const Piece& pc, int hk) {
+    if (pc.t1 == 2) second = ring.request(a, Keys(a, pc.b).bits(KT, KT, ring.lane), pc.b, hk, 1, place ^ 1);
     here = true;
     wait_vm<0>();
     raw_barrier();
@@ -162,16 +162,17 @@ struct Walk {
   // tile(place, valid keys) for every tile of a piece; past(place) behind it.  (No tile is passed over: a way round the products
   // would have the compiler move the accumulators at every tile.)
   template <typename F, typename G>
-  __device__ inline void operator()(Args& a, const Piece& pc, int hk, bool more, const Piece& nx, int next_hk, F tile, G past) {
+  __device__ __forceinline__ void operator()(Args& a, const Piece& pc, int hk, bool more, const Piece& nx, int next_hk, F tile, G past) {
     asked = false;
+    const Keys keys(a, pc.b);
     for (int t = pc.t0; t < pc.t1; ++t) {
       wait_vm<0>();
       raw_barrier();  // the tile is there for all, and all are done with the other place
       const uint64_t now = bits;
       if (t + 1 < pc.t1) {
-        bits = here ? second : ring.request(a, pc.b, hk, t + 1, place ^ 1);
+        bits = here ? second : ring.request(a, keys.bits((t + 1) * KT, KT, ring.lane), pc.b, hk, t + 1, place ^ 1);
       } else if (more && nx.t0 < nx.t1) {
-        bits = ring.request(a, nx.b, next_hk, nx.t0, place ^ 1);
+        bits = ring.request(a, Keys(a, nx.b).bits(nx.t0 * KT, KT, ring.lane), nx.b, next_hk, nx.t0, place ^ 1);
         asked = true;
       }
       tile(place, now);
