@@ -108,12 +108,17 @@ struct Place {
       pair[i] = p - (x == 0 ? 0 : x == 1 ? a.nt : a.nt + a.nh);
     }
   }
+  __device__ inline void weights(const float* from, float w[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = from ? from[(i < 4 ? o0 : o1 - 4) + i] : 1.f;
+  }
   // cosines and sines of raster token n (unturned: 1, 0)
   __device__ inline void angles(const Geom& g, const RopeArgs& a, int n, float cs[4], float sn[4]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
     if (!turns) return;
-    const int w = n % g.Ws, th = n / g.Ws, h = th % g.Hs, t = th / g.Hs;
+    const uint32_t th = (uint32_t)n / (uint32_t)g.Ws, t = th / (uint32_t)g.Hs;
+    const int w = n - (int)th * g.Ws, h = (int)(th - t * (uint32_t)g.Hs);
     const int64_t at[3] = {(int64_t)t * a.nt, (int64_t)g.T * a.nt + (int64_t)h * a.nh,
                            (int64_t)g.T * a.nt + (int64_t)g.Hs * a.nh + (int64_t)w * a.nw};
 #pragma unroll
@@ -146,165 +151,171 @@ __device__ inline int raster_token(const Geom& g, int m) {
   return ((bt * g.Ct + ct) * g.Hs + (bh * g.Ch + ch)) * g.Ws + (bw * g.Cw + cw);
 }
 
+// Rows of the values, which are only moved: HB heads of them in flight.
+template <typename T, int HB>
+__device__ inline void move_rows(const T* from, int64_t fs, T* to, int64_t ts, int h0, int h1) {
+  constexpr int NV = sizeof(T) * 8 / 16;
+  for (int h = h0; h < h1; h += HB) {
+    u32x4 v[HB][NV];
+#pragma unroll
+    for (int j = 0; j < HB; ++j)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) v[j][i] = reinterpret_cast<const u32x4*>(from + min(h + j, h1 - 1) * fs)[i];
+#pragma unroll
+    for (int j = 0; j < HB; ++j)
+      if (h + j < h1)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) reinterpret_cast<u32x4*>(to + (h + j) * ts)[i] = v[j][i];
+  }
+}
+
+// A workgroup has one of the tensors (blockIdx.z counts those that are there), 4 * 64 / LPR rows of the result and a range of heads (blockIdx.y).
+__device__ inline int tensor_of(int have) {  // the blockIdx.z-th bit
+  int z = blockIdx.z;
+  for (int i = 0; i < 3; ++i)
+    if ((have >> i) & 1 && z-- == 0) return i;
+  return 0;
+}
+template <typename P>
+__device__ inline P pick(P const (&p)[3], int z) { return z == 0 ? p[0] : z == 1 ? p[1] : p[2]; }
+
 template <typename T, int LPR, bool HALVES>
-__global__ __launch_bounds__(256) void rope_fwd_kernel(Geom g, RopeArgs a, int heads) {
+__global__ __launch_bounds__(256) void rope_fwd_kernel(Geom g, RopeArgs a, int heads, int have) {
   constexpr int RPW = 64 / LPR, HB = 4;  // rows of a wavefront, heads in flight
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, z = tensor_of(have);
   const Place<LPR, HALVES> pl(g, a, lane);
   const int64_t at = ((int64_t)blockIdx.x * 4 + wave) * RPW + pl.rows_at;  // row of the results, over the batch
   if (at >= (int64_t)g.B * g.L) return;                                   // (a row's lanes leave together)
-  const int b = (int)(at / g.L), m = (int)(at - (int64_t)b * g.L), n = raster_token(g, m);
+  const int b = (int)((uint32_t)at / (uint32_t)g.L), m = (int)at - b * g.L, n = raster_token(g, m);
   const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, g.H);
-  float cs[4], sn[4];
+  const T* X = static_cast<const T*>(pick(a.X, z)) + b * a.x.b + n * a.x.l;
+  T* Y = static_cast<T*>(pick(a.Y, z)) + ((int64_t)b * g.H * g.L + m) * g.d;
+  const int64_t ys = (int64_t)g.L * g.d;
+  if (z == 2) {
+    if (pl.live) move_rows<T, HB>(X + 8 * pl.c, a.x.h, Y + 8 * pl.c, ys, h0, h1);
+    return;
+  }
+  float cs[4], sn[4], w[8];
   pl.angles(g, a, n, cs, sn);
-  const int64_t from = b * a.x.b + n * a.x.l, to = ((int64_t)b * g.H * g.L + m) * g.d;
+  pl.weights(z ? a.w[1] : a.w[0], w);
   const float inv_d = 1.f / g.d;
+  for (int h = h0; h < h1; h += HB) {
+    float x[HB][8];
 #pragma unroll
-  for (int z = 0; z < 2; ++z) {
-    if (!a.X[z]) continue;
-    const T* X = static_cast<const T*>(a.X[z]) + from;
-    T* Y = static_cast<T*>(a.Y[z]) + to;
-    float w[8];
+    for (int j = 0; j < HB; ++j) load8<HALVES>(X + min(h + j, h1 - 1) * a.x.h, pl.o0, pl.o1, x[j]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = a.w[z] ? a.w[z][(i < 4 ? pl.o0 : pl.o1 - 4) + i] : 1.f;
+    for (int j = 0; j < HB; ++j) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[j][i], x[j][i], s);
+      const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<LPR>(pl.live ? s : 0.f), inv_d, a.eps));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[j][i] = x[j][i] * r * w[i];
+      if (pl.turns) turn<HALVES>(x[j], cs, sn, 1.f);
+      if (pl.live && h + j < h1) store8<HALVES>(Y + (h + j) * ys, pl.o0, pl.o1, x[j]);
+    }
+  }
+}
+
+// Backward.  A workgroup takes groups of rows in turn and keeps its share of its tensor's dw in registers; the workgroups' shares
+// are added up by a second launch, in a fixed order.
+template <typename T, int LPR, bool HALVES>
+__global__ __launch_bounds__(256) void rope_bwd_kernel(Geom g, RopeArgs a, int heads, int have) {
+  constexpr int RPW = 64 / LPR, HB = 2;
+  __shared__ float red[4][64][8];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, z = tensor_of(have);
+  const Place<LPR, HALVES> pl(g, a, lane);
+  const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, g.H);
+  const float inv_d = 1.f / g.d;
+  const int64_t rows = (int64_t)g.B * g.L, ys = (int64_t)g.L * g.d;
+  const T* dYz = static_cast<const T*>(pick(a.dY, z));
+  T* dXz = static_cast<T*>(pick(a.dX, z));
+  const T* Xz = static_cast<const T*>(z == 0 ? a.X[0] : a.X[1]);
+  float dw[8], w[8];
+  if (z < 2) pl.weights(z ? a.w[1] : a.w[0], w);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) dw[i] = 0.f;
+  for (int64_t first = ((int64_t)blockIdx.x * 4 + wave) * RPW; first < rows; first += (int64_t)gridDim.x * 4 * RPW) {
+    const int64_t at = first + pl.rows_at;
+    if (at >= rows) continue;
+    const int b = (int)((uint32_t)at / (uint32_t)g.L), m = (int)at - b * g.L, n = raster_token(g, m);
+    const T* dY = dYz + ((int64_t)b * g.H * g.L + m) * g.d;
+    T* dX = dXz + b * a.dx.b + n * a.dx.l;
+    if (z == 2) {
+      if (pl.live) move_rows<T, 4>(dY + 8 * pl.c, ys, dX + 8 * pl.c, a.dx.h, h0, h1);
+      continue;
+    }
+    const T* X = Xz + b * a.x.b + n * a.x.l;
+    float cs[4], sn[4];
+    pl.angles(g, a, n, cs, sn);
     for (int h = h0; h < h1; h += HB) {
-      float x[HB][8];
-#pragma unroll
-      for (int j = 0; j < HB; ++j) load8<HALVES>(X + min(h + j, h1 - 1) * a.x.h, pl.o0, pl.o1, x[j]);
+      float x[HB][8], u[HB][8];
 #pragma unroll
       for (int j = 0; j < HB; ++j) {
+        load8<HALVES>(X + min(h + j, h1 - 1) * a.x.h, pl.o0, pl.o1, x[j]);
+        load8<HALVES>(dY + min(h + j, h1 - 1) * ys, pl.o0, pl.o1, u[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < HB; ++j) {
+        if (pl.turns) turn<HALVES>(u[j], cs, sn, -1.f);
+        const bool there = pl.live && h + j < h1;
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[j][i], x[j][i], s);
         const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<LPR>(pl.live ? s : 0.f), inv_d, a.eps));
+        float t = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[j][i] = x[j][i] * r * w[i];
-        if (pl.turns) turn<HALVES>(x[j], cs, sn, 1.f);
-        if (pl.live && h + j < h1) store8<HALVES>(Y + (int64_t)(h + j) * g.L * g.d, pl.o0, pl.o1, x[j]);
+        for (int i = 0; i < 8; ++i) {
+          x[j][i] *= r;
+          if (there) dw[i] = __builtin_fmaf(u[j][i], x[j][i], dw[i]);
+          u[j][i] *= w[i];
+          t = __builtin_fmaf(u[j][i], x[j][i], t);
+        }
+        t = row_sum<LPR>(pl.live ? t : 0.f) * inv_d;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[j][i] = r * __builtin_fmaf(-x[j][i], t, u[j][i]);
+        if (there) store8<HALVES>(dX + (h + j) * a.dx.h, pl.o0, pl.o1, u[j]);
       }
     }
   }
-  if (a.X[2] && pl.live) {
-    const T* X = static_cast<const T*>(a.X[2]) + from + 8 * pl.c;
-    T* Y = static_cast<T*>(a.Y[2]) + to + 8 * pl.c;
-    constexpr int NV = sizeof(T) * 8 / 16;
-#pragma unroll 4
-    for (int h = h0; h < h1; ++h)
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        reinterpret_cast<u32x4*>(Y + (int64_t)h * g.L * g.d)[i] = reinterpret_cast<const u32x4*>(X + h * a.x.h)[i];
-  }
-}
-
-// Backward.  A workgroup takes groups of rows in turn and keeps its share of dw in registers; the workgroups' sums are added
-// up by a second launch, in a fixed order.
-template <typename T, int LPR, bool HALVES>
-__global__ __launch_bounds__(256) void rope_bwd_kernel(Geom g, RopeArgs a, int heads) {
-  constexpr int RPW = 64 / LPR, HB = 2;
-  __shared__ float red[4][64][8];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Place<LPR, HALVES> pl(g, a, lane);
-  const int h0 = blockIdx.y * heads, h1 = min(h0 + heads, g.H);
-  const float inv_d = 1.f / g.d;
-  float dw[2][8], w[2][8];
-#pragma unroll
-  for (int z = 0; z < 2; ++z)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      dw[z][i] = 0.f;
-      w[z][i] = a.w[z] ? a.w[z][(i < 4 ? pl.o0 : pl.o1 - 4) + i] : 1.f;
-    }
-  const int64_t rows = (int64_t)g.B * g.L;
-  for (int64_t first = ((int64_t)blockIdx.x * 4 + wave) * RPW; first < rows; first += (int64_t)gridDim.x * 4 * RPW) {
-    const int64_t at = first + pl.rows_at;
-    if (at >= rows) continue;
-    const int b = (int)(at / g.L), m = (int)(at - (int64_t)b * g.L), n = raster_token(g, m);
-    float cs[4], sn[4];
-    pl.angles(g, a, n, cs, sn);
-    const int64_t from = b * a.x.b + n * a.x.l, back = b * a.dx.b + n * a.dx.l, to = ((int64_t)b * g.H * g.L + m) * g.d;
-#pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      if (!a.X[z]) continue;
-      const T* X = static_cast<const T*>(a.X[z]) + from;
-      const T* dY = static_cast<const T*>(a.dY[z]) + to;
-      T* dX = static_cast<T*>(a.dX[z]) + back;
-      for (int h = h0; h < h1; h += HB) {
-        float x[HB][8], u[HB][8];
-#pragma unroll
-        for (int j = 0; j < HB; ++j) {
-          load8<HALVES>(X + min(h + j, h1 - 1) * a.x.h, pl.o0, pl.o1, x[j]);
-          load8<HALVES>(dY + (int64_t)min(h + j, h1 - 1) * g.L * g.d, pl.o0, pl.o1, u[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < HB; ++j) {
-          if (pl.turns) turn<HALVES>(u[j], cs, sn, -1.f);
-          const bool there = pl.live && h + j < h1;
-          float s = 0.f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[j][i], x[j][i], s);
-          const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<LPR>(pl.live ? s : 0.f), inv_d, a.eps));
-          float t = 0.f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            x[j][i] *= r;
-            if (there) dw[z][i] = __builtin_fmaf(u[j][i], x[j][i], dw[z][i]);
-            u[j][i] *= w[z][i];
-            t = __builtin_fmaf(u[j][i], x[j][i], t);
-          }
-          t = row_sum<LPR>(pl.live ? t : 0.f) * inv_d;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) u[j][i] = r * __builtin_fmaf(-x[j][i], t, u[j][i]);
-          if (there) store8<HALVES>(dX + (h + j) * a.dx.h, pl.o0, pl.o1, u[j]);
-        }
-      }
-    }
-    if (a.dY[2] && pl.live) {
-      const T* dY = static_cast<const T*>(a.dY[2]) + to + 8 * pl.c;
-      T* dX = static_cast<T*>(a.dX[2]) + back + 8 * pl.c;
-      constexpr int NV = sizeof(T) * 8 / 16;
-#pragma unroll 4
-      for (int h = h0; h < h1; ++h)
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-          reinterpret_cast<u32x4*>(dX + h * a.dx.h)[i] = reinterpret_cast<const u32x4*>(dY + (int64_t)h * g.L * g.d)[i];
-    }
-  }
+  if (z == 2 || !(z ? a.dw[1] : a.dw[0])) return;
   // the workgroup's sums: its 4 * RPW row slots in a fixed order
 #pragma unroll
-  for (int z = 0; z < 2; ++z) {
-    if (!a.dw[z]) continue;
-    __syncthreads();
+  for (int i = 0; i < 8; ++i) red[wave][lane][i] = dw[i];
+  __syncthreads();
+  if (threadIdx.x < LPR && pl.live) {
+    const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    float* out = a.part + (wg * 2 + z) * g.d;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) red[wave][lane][i] = dw[z][i];
-    __syncthreads();
-    if (threadIdx.x < LPR && pl.live) {
-      const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-      float* out = a.part + (wg * 2 + z) * g.d;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float s = 0.f;
-        for (int v = 0; v < 4; ++v)
-          for (int k = 0; k < RPW; ++k) s += red[v][k * LPR + lane][i];
-        out[(i < 4 ? pl.o0 : pl.o1 - 4) + i] = s;
-      }
+    for (int i = 0; i < 8; ++i) {
+      float s = 0.f;
+#pragma unroll 1
+      for (int v = 0; v < 4; ++v)
+        for (int k = 0; k < RPW; ++k) s += red[v][k * LPR + lane][i];
+      out[(i < 4 ? pl.o0 : pl.o1 - 4) + i] = s;
     }
   }
 }
 
-// dw: sums over the workgroups' shares, fp64.  16 channels and 16 shares a workgroup at a time.
-__global__ __launch_bounds__(256) void rope_dw_kernel(const float* part, int n, int d, float* dwq, float* dwk) {
-  __shared__ double red[16][16];
+// dw: sums over the workgroups' shares, fp64.  16 channels and 64 shares a workgroup at a time.
+__global__ __launch_bounds__(1024) void rope_dw_kernel(const float* part, int n, int d, float* dwq, float* dwk) {
+  __shared__ double red[64][16];
   float* out = blockIdx.y ? dwk : dwq;
   if (!out) return;
   const int c = blockIdx.x * 16 + (threadIdx.x & 15), k = threadIdx.x >> 4;
   double s = 0.;
   if (c < d)
 #pragma unroll 8
-    for (int i = k; i < n; i += 16) s += part[((int64_t)i * 2 + blockIdx.y) * d + c];
+    for (int i = k; i < n; i += 64) s += part[((int64_t)i * 2 + blockIdx.y) * d + c];
   red[k][threadIdx.x & 15] = s;
   __syncthreads();
+  if (k < 8) {
+    for (int i = 1; i < 8; ++i) s += red[8 * i + k][threadIdx.x & 15];
+    red[k][threadIdx.x & 15] = s;  // (row k is read by this thread alone above)
+  }
+  __syncthreads();
   if (k == 0 && c < d) {
-    for (int i = 1; i < 16; ++i) s += red[i][threadIdx.x & 15];
+    for (int i = 1; i < 8; ++i) s += red[i][threadIdx.x & 15];
     out[c] = (float)s;
   }
 }
@@ -321,7 +332,7 @@ __global__ __launch_bounds__(256) void rope_table_kernel(Geom g, int nt, int nh,
   }
 }
 
-constexpr int kBwdGroups = 2048;  // workgroups of a backward launch at most (two a SIMD): each leaves 2 d sums
+constexpr int kBwdGroups = 1024;  // workgroups of a tensor's backward at most: each leaves d sums
 
 // Heads of a workgroup and workgroups along them: all heads, unless that leaves the chip short of wavefronts.
 static int head_split(int64_t groups, int H) {
@@ -349,21 +360,26 @@ size_t rope_bwd_workspace(const Geom& g) {
 
 template <typename T, int LPR, bool HALVES>
 static int launch_t(const Geom& g, const RopeArgs& a, bool backward, hipStream_t st) {
-  int heads;
-  if (backward) {
-    const dim3 grid = bwd_grid(g, &heads);
-    hipLaunchKernelGGL((rope_bwd_kernel<T, LPR, HALVES>), grid, dim3(256), 0, st, g, a, heads);
-    if (const int rc = check_launch()) return rc;
-    if (a.dw[0] || a.dw[1]) {
-      hipLaunchKernelGGL(rope_dw_kernel, dim3((g.d + 15) / 16, 2), dim3(256), 0, st, a.part, (int)(grid.x * grid.y), g.d, a.dw[0], a.dw[1]);
-      return check_launch();
+  int heads, have = 0, tensors = 0;
+  for (int i = 0; i < 3; ++i)
+    if (backward ? a.dY[i] != nullptr : a.X[i] != nullptr) {
+      have |= 1 << i;
+      ++tensors;
     }
-    return BSA_OK;
+  if (backward) {
+    dim3 grid = bwd_grid(g, &heads);
+    const int shares = (int)(grid.x * grid.y);
+    grid.z = tensors;
+    hipLaunchKernelGGL((rope_bwd_kernel<T, LPR, HALVES>), grid, dim3(256), 0, st, g, a, heads, have);
+    if (const int rc = check_launch()) return rc;
+    if (!a.dw[0] && !a.dw[1]) return BSA_OK;
+    hipLaunchKernelGGL(rope_dw_kernel, dim3((g.d + 15) / 16, 2), dim3(1024), 0, st, a.part, shares, g.d, a.dw[0], a.dw[1]);
+    return check_launch();
   }
   constexpr int RPW = 64 / LPR;
   const int64_t groups = ((int64_t)g.B * g.L + 4 * RPW - 1) / (4 * RPW);
   heads = head_split(groups, g.H);
-  hipLaunchKernelGGL((rope_fwd_kernel<T, LPR, HALVES>), dim3((unsigned)groups, (g.H + heads - 1) / heads), dim3(256), 0, st, g, a, heads);
+  hipLaunchKernelGGL((rope_fwd_kernel<T, LPR, HALVES>), dim3((unsigned)groups, (g.H + heads - 1) / heads, tensors), dim3(256), 0, st, g, a, heads, have);
   return check_launch();
 }
 
