@@ -371,9 +371,10 @@ def _strides(t: torch.Tensor, l: int, h: int) -> StridesStruct:
 
 def _device(t: torch.Tensor) -> torch.device:
     """The device of a call: it has to be the current one, whose stream the work goes to."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors must be on the current GPU, not on {t.device}")
-    return t.device
+    device = t.device
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors must be on the current GPU, not on {device}")
+    return device
 
 
 def _take(t: Optional[torch.Tensor], name: str, size, dtype, device, dense: bool = False) -> Optional[int]:
@@ -382,7 +383,7 @@ def _take(t: Optional[torch.Tensor], name: str, size, dtype, device, dense: bool
         return None
     if t.shape != size or t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be {tuple(size)} {dtype} on {device}, not {tuple(t.shape)} {t.dtype} on {t.device}")
-    if dense and not t.is_contiguous() or t.stride(-1) != 1 and t.shape[-1] > 1:
+    if not t.is_contiguous() and (dense or t.stride(-1) != 1 and t.shape[-1] > 1):
         raise ValueError(f"{name} must be contiguous" if dense else f"{name}: the channels of a head must be adjacent")
     return t.data_ptr()
 
@@ -408,10 +409,11 @@ def rope_table(shape: Shape, rope: Rope, theta: float = 10000.0, origin=(0, 0, 0
     return out
 
 
-def _rope_table_ptr(shape: Shape, rope: Optional[Rope], table: Optional[torch.Tensor], device) -> Optional[int]:
+def _rope_table_ptr(shape, rope, table: Optional[torch.Tensor], device) -> Optional[int]:
+    """shape, rope: the C structures' references."""
     if rope is None or table is None or table.numel() == 0:
         return None
-    need = lib().bsa_rope_table_bytes(C.byref(shape.c()), C.byref(rope.c())) // 4
+    need = lib().bsa_rope_table_bytes(shape, rope) // 4
     if table.dtype != torch.float32 or table.device != device or not table.is_contiguous() or table.numel() < need:
         raise ValueError(f"table must be {need} contiguous floats on {device}")
     return table.data_ptr()
@@ -421,8 +423,9 @@ def _same_strides(tensors, names):
     """The common strides of the [B, L, H, d] tensors that are there (an extent of 1 has none)."""
     there = [t for t in tensors if t is not None]
     first = there[0]
+    strides = first.stride()
     for t in there[1:]:
-        if any(a != b and n > 1 for a, b, n in zip(t.stride(), first.stride(), first.shape)):
+        if t.stride() != strides and any(a != b and n > 1 for a, b, n in zip(t.stride(), strides, first.shape)):
             raise ValueError(f"{names} must have the same strides")
     return C.byref(_strides(first, 1, 2))
 
@@ -439,8 +442,8 @@ def qk_norm_rope_fwd(shape: Shape, rope: Optional[Rope], table: Optional[torch.T
     args = [_take(x, n, size_in, dt, dev) for x, n in zip(X, ("Xq", "Xk", "Xv"))]
     w = [_take(t, n, (shape.d,), torch.float32, dev, True) for t, n in ((wq, "wq"), (wk, "wk"))]
     outs = [_take(y, n, size_out, dt, dev, True) for y, n in zip(Y, "QKV")]
-    rp = C.byref(rope.c()) if rope is not None else None
-    st = lib().bsa_qk_norm_rope_fwd(C.byref(shape.c()), rp, _rope_table_ptr(shape, rope, table, dev), *args,
+    sp, rp = C.byref(shape.c()), C.byref(rope.c()) if rope is not None else None
+    st = lib().bsa_qk_norm_rope_fwd(sp, rp, _rope_table_ptr(sp, rp, table, dev), *args,
                                     _same_strides(X, "Xq, Xk and Xv"), *w, eps, *outs, _stream())
     _check(st, "bsa_qk_norm_rope_fwd")
     return tuple(Y)
@@ -466,9 +469,9 @@ def qk_norm_rope_bwd(shape: Shape, rope: Optional[Rope], table: Optional[torch.T
     ys = [_take(t, n, size_y, dt, dev, True) for t, n in zip(dY, ("dQ", "dK", "dV"))]
     outs = [_take(t, n, size_x, dt, dev) for t, n in zip(dX, ("dXq", "dXk", "dXv"))]
     dws = [_take(t, n, (shape.d,), torch.float32, dev, True) for t, n in zip(dw, ("dwq", "dwk"))]
-    workspace = _scratch(workspace, qk_norm_rope_bwd_workspace_bytes(shape), dev)
-    rp = C.byref(rope.c()) if rope is not None else None
-    st = lib().bsa_qk_norm_rope_bwd(C.byref(shape.c()), rp, _rope_table_ptr(shape, rope, table, dev), *xs,
+    sp, rp = C.byref(shape.c()), C.byref(rope.c()) if rope is not None else None
+    workspace = _scratch(workspace, lib().bsa_qk_norm_rope_bwd_workspace_bytes(sp), dev)
+    st = lib().bsa_qk_norm_rope_bwd(sp, rp, _rope_table_ptr(sp, rp, table, dev), *xs,
                                     _same_strides(X, "Xq and Xk") if any(t is not None for t in X) else None, *w, eps, *ys, *outs,
                                     _same_strides(dX, "dXq, dXk and dXv"), *dws, _ptr(workspace),
                                     workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())

@@ -471,7 +471,7 @@ int bsa_cross_attn_fwd(const bsa_cross_shape_t* shape, const void* Q, const void
   const size_t need = cross_fwd_workspace(a);
   if (need && (!workspace || workspace_bytes < need)) return BSA_ERR_WORKSPACE;
   a.Q = Q; a.K = K; a.V = V; a.kv_len = kv_len; a.kv_mask = kv_mask; a.sm_scale = sm_scale;
-  a.O_out = O; a.LSE_out = LSE; a.ws = workspace;
+  a.O_out = O; a.LSE_out = LSE; a.ws = workspace; a.ws_bytes = workspace ? workspace_bytes : 0;
   return launch_cross_fwd(a, (hipStream_t)stream);
 }
 
@@ -502,7 +502,7 @@ int bsa_cross_attn_bwd(const bsa_cross_shape_t* shape, const void* Q, const void
     return rc;
   if (!workspace || workspace_bytes < cross_bwd_workspace(a)) return BSA_ERR_WORKSPACE;
   a.Q = Q; a.K = K; a.V = V; a.O = O; a.LSE_in = LSE; a.dO = dO; a.kv_len = kv_len; a.kv_mask = kv_mask;
-  a.sm_scale = sm_scale; a.dQ = dQ; a.dK = dK; a.dV = dV; a.ws = workspace;
+  a.sm_scale = sm_scale; a.dQ = dQ; a.dK = dK; a.dV = dV; a.ws = workspace; a.ws_bytes = workspace_bytes;
   return launch_cross_bwd(a, (hipStream_t)stream);
 }
 

@@ -190,6 +190,7 @@ struct CrossArgs {
   float sm_scale;
   int near;  // 64 rows of every tensor that is streamed lie within 2^31 bytes
   void* ws;
+  size_t ws_bytes;
 };
 size_t cross_fwd_workspace(const CrossArgs& a);
 size_t cross_bwd_workspace(const CrossArgs& a);

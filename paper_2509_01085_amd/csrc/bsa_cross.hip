@@ -798,30 +798,34 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_dkv_combine_kernel(CrossArgs,
 // ---- host ----
 static int padded_d(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// Forward and dQ: two workgroups a CU where registers and LDS allow it.  Shares where whole units would leave workgroups without work for
-// the time of kWorth tiles: what shares cost, the reckoning and the second launch, is about 14 us, a tile 1.2.
-constexpr int kWorth = 12;
+// Forward and dQ: two workgroups a CU where registers and LDS allow it.  Shares where whole units would leave slots without work for
+// the time of `worth` tiles, which is what shares cost: the reckoning, the second launch, and at d = 128 a loop with fewer registers.
+// bf16: about 14 us, a tile takes 1.2.  fp32: 10 to 30 us, a tile 3 to 6, and one workgroup keeps a CU's matrix cores as busy as two, so
+// the CUs are counted, and shares taken only where half of them would have no unit.  4 heads of 64 channels, 700 queries, 200 states in fp32: 59 us whole, 31 in shares; 12 of 128, 2,520 queries, 333
+// states (240 units): 193 and 257; 48 of 1,200 queries, 2,000 states (480 units): 1,630 and 2,070.  Lengths are known on the device only and do not count here: shares for a batch of four of any length
+// up to 2,000 (bf16, 480 units) took 204 us, whole units 128.
 static Deal rows_deal(const CrossArgs& a) {
+  const bool f32 = a.dtype == BSA_F32;
   Deal d{};
-  d.tile = a.dtype == BSA_BF16 && a.d <= 128 ? 64 : 32;  // key_tile
+  d.tile = !f32 && a.d <= 128 ? 64 : 32;  // key_tile
   d.rows = a.Hkv * ((a.M + kUnitRows - 1) / kUnitRows);
   const int64_t units = (int64_t)d.rows * a.B, tiles = (a.S + d.tile - 1) / d.tile;
-  const int slots = a.d <= 128 ? 512 : 256;
+  const int slots = !f32 && a.d <= 128 ? 512 : 256, worth = f32 ? 4 : 12, least = f32 ? 1 : 4;  // (tiles of a share)
   const int64_t idle = ((units + slots - 1) / slots * slots - units) * tiles;  // of all slots together
-  d.way = units < 2 * slots && idle > (int64_t)kWorth * slots ? SHARES : EACH;
-  d.grid = (int)(d.way == SHARES ? std::min<int64_t>(slots, std::max<int64_t>(1, units * tiles / 4)) : units);
+  d.way = units < (f32 ? slots / 2 : 2 * slots) && idle > (int64_t)worth * slots ? SHARES : EACH;
+  d.grid = (int)(d.way == SHARES ? std::min<int64_t>(slots, std::max<int64_t>(1, units * tiles / least)) : units);
   return d;
 }
 
+// A step is worth a share of its own: 8 steps of 2 units in fp32 took 27 us in four shares, 17 in eight, 12 in sixteen.
 static Deal keys_deal(const CrossArgs& a) {
   Deal d{};
   d.by_keys = 1;
   d.tile = kUnitRows;
   d.steps = a.G * query_tiles(a.Lq);
   d.rows = a.Hkv * ((a.S + kUnitRows - 1) / kUnitRows);
-  const int64_t units = (int64_t)d.rows * a.B;
   d.way = SHARES;
-  d.grid = (int)std::min<int64_t>(256, std::max<int64_t>(units, units * d.steps / 4));
+  d.grid = (int)std::min<int64_t>(256, (int64_t)d.rows * a.B * d.steps);
   return d;
 }
 
@@ -844,6 +848,7 @@ size_t cross_bwd_workspace(const CrossArgs& a) {
 template <typename T, int DP>
 static int fwd_t(const CrossArgs& a, hipStream_t st) {
   const Deal d = rows_deal(a);
+  if (part_bytes(d, DP / 2 + 2) > a.ws_bytes) return BSA_ERR_WORKSPACE;
   constexpr size_t lds = 4 * key_tile<T, DP>() * DP * sizeof(T);
   const bool one = d.way == EACH;
   if (const int rc = one ? allow_dynamic_lds<cross_fwd_kernel<T, DP, true>>(lds) : allow_dynamic_lds<cross_fwd_kernel<T, DP, false>>(lds)) return rc;
@@ -858,6 +863,7 @@ static int fwd_t(const CrossArgs& a, hipStream_t st) {
 template <typename T, int DP>
 static int bwd_t(const CrossArgs& a, hipStream_t st) {
   const Deal d = rows_deal(a), k = keys_deal(a);
+  if (stat_bytes(a) + std::max(part_bytes(d, DP / 2), part_bytes(k, DP)) > a.ws_bytes) return BSA_ERR_WORKSPACE;
   constexpr size_t lds = 4 * key_tile<T, DP>() * DP * sizeof(T), klds = 2 * (64 * DP * sizeof(T) + 256);
   const bool one = d.way == EACH;
   if (const int rc = one ? allow_dynamic_lds<cross_dq_kernel<T, DP, true>>(lds) : allow_dynamic_lds<cross_dq_kernel<T, DP, false>>(lds)) return rc;
