@@ -54,22 +54,11 @@ template <> struct Elt<uint16_t> {
 };
 template <> struct Elt<float> {
   using Frag = f32x4;
-  struct Frag8 { float v[8]; };
   static constexpr int CE = 4;
   static __device__ inline Frag zero() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
   static __device__ inline void mma(f32x16& d, const Frag& a, const Frag& b) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], d, 0, 0, 0);
-  }
-  static __device__ inline void mma8(f32x16& d, const Frag8& a, const Frag8& b) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i], b.v[i], d, 0, 0, 0);
-  }
-  static __device__ inline Frag8 column(const f32x16& d, int h) {
-    Frag8 f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f.v[i] = d[8 * h + i];
-    return f;
   }
   static __device__ inline float dot(const Frag& a, const Frag& b) {
     float s = 0.f;
@@ -100,26 +89,48 @@ struct TileView {
     const int r = row0 + (lane & 31), c = 2 * s + (lane >> 5);
     return *reinterpret_cast<const typename E::Frag*>(tile + r * RB + ((c ^ tile_swz<T, DP>(r)) << 4));
   }
-  // rows row0 + 16 h + 8 (t / 4) + 4 grp + t % 4, t = 0..7, of channel 32 dt + col; row0 a multiple of 16
-  __device__ inline typename E::Frag8 along(const uint8_t* tile, int row0, int dt) const {
-    const int grp = lane >> 5;
+  // bf16: rows row0 + 8 (t / 4) + 4 grp + t % 4, t = 0..7, of channel 32 dt + col; row0 a multiple of 16
+  __device__ inline auto along(const uint8_t* tile, int row0, int dt) const {
+    const int grp = lane >> 5, L16 = lane & 15, q16 = lane >> 4, rsub = L16 >> 2, jj = L16 & 3, cl = 2 * (q16 & 1) + (jj >> 1);
+    const int r = row0 + 4 * grp + rsub, c = 4 * dt + cl;
+    const uint8_t* p0 = tile + r * RB + ((c ^ tile_swz<T, DP>(r)) << 4) + 8 * (jj & 1);
+    const uint8_t* p1 = tile + (r + 8) * RB + ((c ^ tile_swz<T, DP>(r + 8)) << 4) + 8 * (jj & 1);
+    return typename E::Frag8{lds_frag_tr(p0, p1)};
+  }
+  // D[dt] += channels 32 dt .. 32 dt + 31 of rows row0 .. row0 + 31 (a multiple of 32) times x, whose element r stands for row d_row(r).
+  // fp32: a value is one product's operand, and a product takes no longer than a value from LDS.  They run eight ahead of the products,
+  // neighbours of which add to different accumulators.  (Row r has its chunks at c ^ (8 grp | r % 8): the address of row
+  // 16 h + 8 a + 4 grp + e is that of 8 a + 4 grp + e and a constant, and a channel tile an exclusive or of bit 7 and a constant.)
+  __device__ inline void gather(f32x16 (&acc)[DP / 32], const uint8_t* tile, int row0, const f32x16& x) const {
+    constexpr int DT = DP / 32;
     if constexpr (sizeof(T) == 2) {
-      const int L16 = lane & 15, q16 = lane >> 4, rsub = L16 >> 2, jj = L16 & 3, cl = 2 * (q16 & 1) + (jj >> 1);
-      const int r = row0 + 4 * grp + rsub, c = 4 * dt + cl;
-      const uint8_t* p0 = tile + r * RB + ((c ^ tile_swz<T, DP>(r)) << 4) + 8 * (jj & 1);
-      const uint8_t* p1 = tile + (r + 8) * RB + ((c ^ tile_swz<T, DP>(r + 8)) << 4) + 8 * (jj & 1);
-      return {lds_frag_tr(p0, p1)};
-    } else {
-      typename E::Frag8 f;
-      int own = lane;  // (not known to the compiler: eight addresses a channel tile, held over the walk, would fill the registers)
-      asm volatile("" : "+v"(own));
-      const int ch = 32 * dt + (own & 31);
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const int r = row0 + 8 * (t >> 2) + 4 * (own >> 5) + (t & 3);
-        f.v[t] = *reinterpret_cast<const float*>(tile + r * RB + (((ch >> 2) ^ tile_swz<T, DP>(r)) << 4) + 4 * (ch & 3));
+      for (int h = 0; h < 2; ++h) {
+        const auto b = E::column(x, h);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) E::mma8(acc[dt], along(tile, row0 + 16 * h, dt), b);
       }
-      return f;
+    } else {
+      constexpr int AHEAD = 8, N = 16 * DT;
+      const int grp = lane >> 5, col = lane & 31;
+      int at[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+        at[t] = row0 * RB + (8 * (t >> 2) + 4 * grp + (t & 3)) * RB + ((((col >> 2) ^ (t & 7)) | (grp << 3)) << 4) + 4 * (col & 3);
+      auto value = [&](int n) {
+        const int r = n / DT, dt = n % DT;
+        return *reinterpret_cast<const float*>(tile + (at[r & 7] ^ ((dt & 1) << 7)) + (r >> 3) * 16 * RB + (dt >> 1) * 256);
+      };
+      float f[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) f[n] = value(n);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        acc[n % DT] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[n % AHEAD], x[n / DT], acc[n % DT], 0, 0, 0);
+        if (n + AHEAD < N) f[n % AHEAD] = value(n + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
 };

@@ -68,8 +68,17 @@ struct RowFrags {
   // D += rows row0 .. row0 + 31 of the tile times this
   __device__ inline void times(f32x16& acc, const TileView<T, DP>& view, const uint8_t* tile, int row0) const {
     if constexpr (HELD) {
+      constexpr int AHEAD = sizeof(T) == 4 ? 2 : 4;  // (fp32: four products a fragment)
+      typename E::Frag fr[AHEAD];
 #pragma unroll
-      for (int s = 0; s < DS; ++s) E::mma(acc, view.row(tile, row0, s), f[s]);
+      for (int s = 0; s < AHEAD; ++s) fr[s] = view.row(tile, row0, s);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < DS; ++s) {
+        E::mma(acc, fr[s % AHEAD], f[s]);
+        if (s + AHEAD < DS) fr[s % AHEAD] = view.row(tile, row0, s + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     } else {
       const int n = (d / E::CE + 1) / 2;
       typename E::Frag f[2] = {row_chunk(p, grp, live, d), row_chunk(p, 2 + grp, live, d)};
@@ -96,7 +105,8 @@ struct RowFrags {
     return sum;
   }
 };
-template <typename T, int DP> constexpr int two_a_cu() { return DP <= 128 ? 2 : 1; }
+// Workgroups of a CU: dQ in fp32 with 128 channels (Q, dO, dQ in registers) and the walk over several pieces of such rows have one.
+template <typename T, int DP, bool LEAN> constexpr int a_cu() { return DP <= 128 && (LEAN || DP * sizeof(T) <= 256) ? 2 : 1; }
 template <typename T, int DP> constexpr bool held() { return DP <= 128; }
 
 // ---- forward ----
@@ -282,8 +292,7 @@ __device__ inline void fwd_tile(Walked<D / 32>& w, const Fragments<D>& fg, const
 
 // ONE: a unit a workgroup (Deal::EACH), without what the walk over several pieces needs.
 template <typename T, int DP, bool ONE>
-__global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_fwd_kernel(CrossArgs, Deal dl, float* part) {
-  using E = Elt<T>;
+__global__ __launch_bounds__(kThreads, (a_cu<T, DP, ONE>())) void cross_fwd_kernel(CrossArgs, Deal dl, float* part) {
   using Ring = KvRing<T, DP>;
   constexpr int KT = key_tile<T, DP>(), NK = KT / 32, DT = DP / 32;
   extern __shared__ __align__(16) uint8_t smem[];  // [2][K tile | V tile]
@@ -325,7 +334,6 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_fwd_kerne
       walk(a, pc, u.hk, more, nx, key_head(a, nx.unit),
            [&](int place, uint64_t now) {
              any |= now != 0;
-             if (!u.any || now == 0) return;
              f32x16 s[NK];
 #pragma unroll
              for (int k = 0; k < NK; ++k) {
@@ -336,13 +344,7 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_fwd_kerne
              if (now != Ring::ALL) mask_logits<NK>(s, now >> (4 * grp));
              w.template softmax<NK>(s, c);
 #pragma unroll
-             for (int k = 0; k < NK; ++k)
-#pragma unroll
-               for (int h = 0; h < 2; ++h) {
-                 const auto p = E::column(s[k], h);
-#pragma unroll
-                 for (int dt = 0; dt < DT; ++dt) E::mma8(w.o[dt], view.along(ring.v_tile(place), 32 * k + 16 * h, dt), p);
-               }
+             for (int k = 0; k < NK; ++k) view.gather(w.o, ring.v_tile(place), 32 * k, s[k]);
            },
            [](int) {});
     }
@@ -535,8 +537,7 @@ __device__ inline float delta_tile(const Fragments<D>& fg, const bf16x8* q, cons
 }
 
 template <typename T, int DP, bool ONE>
-__global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel(CrossArgs, Deal dl, float* stat, float* part) {
-  using E = Elt<T>;
+__global__ __launch_bounds__(kThreads, (a_cu<T, DP, false>())) void cross_dq_kernel(CrossArgs, Deal dl, float* stat, float* part) {
   using Ring = KvRing<T, DP>;
   constexpr int KT = key_tile<T, DP>(), NK = KT / 32, DT = DP / 32;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -554,7 +555,7 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel
     const RowUnit u(a, pc.b, pc.unit, wave, lane);
     walk.ask(a, pc, u.hk);
     RowFrags<T, DP, held<T, DP>()> q;
-    RowFrags<T, DP, held<T, DP>() && DP * sizeof(T) <= 256> gr;  // (fp32, 128 channels: Q, dQ and this are more than two workgroups' share)
+    RowFrags<T, DP, held<T, DP>()> gr;
     q.load(static_cast<const T*>(a.Q) + u.offset(a, a.q), u.live, a.d, grp);
     gr.load(static_cast<const T*>(a.dO) + u.offset(a, a.go), u.live, a.d, grp);
     const float lse2 = u.live ? a.LSE_in[u.flat(a)] * kLog2e : INFINITY;
@@ -594,7 +595,6 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel
       const TileView<T, DP> view(lane);
       walk(a, pc, u.hk, more, nx, key_head(a, nx.unit),
            [&](int place, uint64_t now) {
-             if (!u.any || now == 0) return;
 #pragma unroll
              for (int k = 0; k < NK; ++k) {
                f32x16 s, dp;
@@ -607,12 +607,7 @@ __global__ __launch_bounds__(kThreads, (two_a_cu<T, DP>())) void cross_dq_kernel
                if (now != Ring::ALL) mask_weights(s, now >> (32 * k + 4 * grp));
 #pragma unroll
                for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
-#pragma unroll
-               for (int h = 0; h < 2; ++h) {
-                 const auto ds = E::column(s, h);
-#pragma unroll
-                 for (int dt = 0; dt < DT; ++dt) E::mma8(dq[dt], view.along(ring.k_tile(place), 32 * k + 16 * h, dt), ds);
-               }
+               view.gather(dq, ring.k_tile(place), 32 * k, s);
              }
            },
            [](int) {});
@@ -665,7 +660,6 @@ enum { BOTH = 0, ONLY_K = 1, ONLY_V = 2 };
 
 template <typename T, int DP, int WHAT>
 __device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) {
-  using E = Elt<T>;
   constexpr int DT = DP / 32, TILE = 32 * DP * sizeof(T), STAGE = 2 * TILE + 256;
   constexpr bool WITH_K = WHAT != ONLY_V, WITH_V = WHAT != ONLY_K;
   extern __shared__ __align__(16) uint8_t smem[];  // [2][Q tile | dO tile | LSE, -delta]
@@ -715,11 +709,10 @@ __device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) 
     if (tid < 16) dma16(stat + (((int64_t)u.b * a.H + head) * tiles + i) * 64 + 4 * tid, at + 2 * TILE);
   };
   if (t0 < t1) request(t0);
-  for (int t = t0; t < t1; ++t) {
+  for (int t = t0; t < t1; ++t) {  // (a way round the products, for a wavefront without valid keys, would move the accumulators every time)
     wait_vm<0>();
     raw_barrier();
     if (t + 1 < t1) request(t + 1);
-    if (mine == 0) continue;
     const uint8_t* qt = smem + (t & 1) * STAGE;
     const uint8_t* gt = qt + TILE;
     const f32x4* st = reinterpret_cast<const f32x4*>(qt + 2 * TILE) + grp;
@@ -738,19 +731,8 @@ __device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) 
         dp[r] = s[r] * (dp[r] + nd[e]);
       }
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if constexpr (WITH_V) {
-        const auto p = E::column(s, h);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) E::mma8(dv[dt], view.along(gt, 16 * h, dt), p);
-      }
-      if constexpr (WITH_K) {
-        const auto ds = E::column(dp, h);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) E::mma8(dk[dt], view.along(qt, 16 * h, dt), ds);
-      }
-    }
+    if constexpr (WITH_V) view.gather(dv, gt, 0, s);
+    if constexpr (WITH_K) view.gather(dk, qt, 0, dp);
   }
   // what a key that is not valid has gathered is no number of its own: its gradient is zero
   auto put = [&](const f32x16 (&acc)[DT], void* to, const __attribute__((address_space(4))) bsa_strides_t& st, float scale, int place) {
