@@ -105,6 +105,11 @@ def parse():
     ap.add_argument("--length-sweep", action="store_true",
                     help="speedup over the in-repo dense kernel versus sequence length (forward only and forward + "
                          "backward), one JSON line per length, at the paper's token counts from 23K to 153K")
+    ap.add_argument("--block", action="store_true",
+                    help="the attention part of a transformer block on the workload's shape instead: norm and rotation of a packed "
+                         "projection, sparse self-attention in block-major order, cross attention to --states encoder states, forward "
+                         "and backward; one JSON line with the time of every call")
+    ap.add_argument("--states", type=int, default=512, help="encoder states of --block")
     ap.add_argument("--calibration-copy-mib", type=int, default=0,
                     help="also run one plain elementwise copy of this many MiB (read + write that much each), "
                          "the known-traffic dispatch that hardware-counter readings are scaled by")
@@ -278,6 +283,102 @@ def length_sweep(args, torch, B):
             del x, Q, K, V, dO, O, dQ, dK, dV, lists, ws, fws
 
 
+class BlockAttention:
+    """The attention part of a transformer block, forward and backward, on one GPU: the projection's queries, keys and values
+    [B, L, 3, H, d] are normalised, rotated and brought to block-major [B, H, L, d]; sparse self-attention; cross attention of queries
+    [B, L, H, d] of a second projection to the packed keys and values [B, states, 2, H, d] of an encoder.  The projections themselves are
+    the caller's.  Every buffer is allocated here, once."""
+
+    EPS = 1e-6
+
+    def __init__(self, wl, states, torch, B, kv_len=None):
+        self.wl, self.B = wl.replace(block_major=True), B
+        dt = torch.float32 if wl.dtype == "fp32" else torch.bfloat16
+        x = make_inputs(wl.replace(block_major=False), torch)
+        dev = x["Q"].device
+        gen = torch.Generator(device=dev).manual_seed(wl.seed)
+        rand = lambda *s, to=dt: torch.randn(s, generator=gen, device=dev).to(to)  # noqa: E731
+        new = lambda *s, to=dt: torch.empty(s, dtype=to, device=dev)  # noqa: E731
+        b, h, n, d = wl.B, wl.H, wl.L, wl.d
+        self.shape = B.Shape(b, h, *wl.grid, *wl.block, d, B.F32 if wl.dtype == "fp32" else B.BF16, *wl.window, 1)
+        hw = d // 6 * 2
+        self.rope = B.Rope(d - 2 * hw, hw, hw)
+        self.table = B.rope_table(self.shape, self.rope)
+        self.X = torch.stack([x[k].transpose(1, 2) for k in "QKV"], 2)
+        self.wq, self.wk = (1.0 + 0.1 * rand(d, to=torch.float32) for _ in range(2))
+        self.cross = B.CrossShape(b, h, h, n, states, d, self.shape.dtype)
+        self.Xc, self.KV, self.kv_len = rand(b, n, h, d), rand(b, states, 2, h, d), kv_len
+        self.dO, self.dOc = rand(b, h, n, d), rand(b, n, h, d)
+        self.Q, self.K, self.V, self.O, self.dQ, self.dK, self.dV = (new(b, h, n, d) for _ in range(7))
+        self.Oc, self.dXc, self.dKV, self.dX = new(b, n, h, d), new(b, n, h, d), torch.empty_like(self.KV), torch.empty_like(self.X)
+        self.LSE, self.LSEc = new(b, h, n, to=torch.float32), new(b, h, n, to=torch.float32)
+        self.dwq, self.dwk = new(d, to=torch.float32), new(d, to=torch.float32)
+        nk = B.n_keep(self.shape, wl.keep_ratio)
+        self.Qbar, self.Kbar = (new(b, h, self.shape.N, d, to=torch.float64) for _ in range(2))
+        self.lists, self.keep = B.alloc_kv_lists(self.shape, dev), new(b, h, self.shape.N, nk, to=torch.int32)
+        space = lambda nbytes: new(max(1, nbytes), to=torch.uint8)  # noqa: E731
+        c = self.cross
+        self.ws = {"rope": space(B.qk_norm_rope_bwd_workspace_bytes(self.shape)), "fwd": space(B.fwd_workspace_bytes(self.shape, nk)),
+                   "bwd": space(B.bwd_workspace_bytes(self.shape, nk)), "cfwd": space(B.cross_fwd_workspace_bytes(c)),
+                   "cbwd": space(B.cross_bwd_workspace_bytes(c))}
+
+    def norm_rope_fwd(self):
+        self.B.qk_norm_rope_fwd(self.shape, self.rope, self.table, *self.X.unbind(2), wq=self.wq, wk=self.wk, eps=self.EPS,
+                                Q=self.Q, K=self.K, V=self.V)
+
+    def indices(self):
+        self.B.pool_blocks(self.shape, self.Q, self.Qbar)
+        self.B.pool_blocks(self.shape, self.K, self.Kbar)
+        self.B.select_kv(self.shape, self.Qbar, self.Kbar, self.wl.threshold, out=self.lists)
+        self.B.prune_q(self.shape, self.Q, self.wl.keep_ratio, self.keep)
+
+    def attn_fwd(self):
+        self.B.attn_fwd(self.shape, self.Q, self.K, self.V, self.lists, self.keep, O=self.O, LSE=self.LSE, workspace=self.ws["fwd"])
+
+    def attn_bwd(self):
+        self.B.attn_bwd(self.shape, self.Q, self.K, self.V, self.O, self.LSE, self.dO, self.lists, self.keep, dQ=self.dQ, dK=self.dK,
+                        dV=self.dV, workspace=self.ws["bwd"])
+
+    def _cross(self):
+        heads = lambda t: t.transpose(1, 2)  # noqa: E731
+        return heads, heads(self.Xc), *(heads(t) for t in self.KV.unbind(2))
+
+    def cross_fwd(self):
+        heads, Q, K, V = self._cross()
+        self.B.cross_attn_fwd(self.cross, Q, K, V, kv_len=self.kv_len, O=heads(self.Oc), LSE=self.LSEc, workspace=self.ws["cfwd"])
+
+    def cross_bwd(self):
+        heads, Q, K, V = self._cross()
+        self.B.cross_attn_bwd(self.cross, Q, K, V, heads(self.Oc), self.LSEc, heads(self.dOc), kv_len=self.kv_len, dQ=heads(self.dXc),
+                              dK=heads(self.dKV[:, :, 0]), dV=heads(self.dKV[:, :, 1]), workspace=self.ws["cbwd"])
+
+    def norm_rope_bwd(self):
+        dX = self.dX.unbind(2)
+        self.B.qk_norm_rope_bwd(self.shape, self.rope, self.table, self.X[:, :, 0], self.X[:, :, 1], self.dQ, self.dK, self.dV, wq=self.wq,
+                                wk=self.wk, eps=self.EPS, dXq=dX[0], dXk=dX[1], dXv=dX[2], dwq=self.dwq, dwk=self.dwk,
+                                workspace=self.ws["rope"])
+
+    CALLS = ("norm_rope_fwd", "indices", "attn_fwd", "cross_fwd", "cross_bwd", "attn_bwd", "norm_rope_bwd")
+
+    def step(self):
+        for name in self.CALLS:
+            getattr(self, name)()
+
+
+def block(args, wl, torch, B):
+    b = BlockAttention(wl, args.states, torch, B)
+    for _ in range(max(1, args.warmup)):
+        b.step()
+    ms, median = timed_each(torch, b.step, args.steps)
+    parts = {name: timed(torch, getattr(b, name), args.steps) for name in b.CALLS}
+    print(json.dumps({
+        "metric": "block_attention_fwd_bwd_ms", "value": ms, "unit": "ms", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+        "ms_per_step": ms, "ms_per_step_median": median, "higher_is_better": False, "dtype": wl.dtype, "data": "synthetic",
+        "config": {"workload": wl.name, "B": wl.B, "H": wl.H, "d": wl.d, "grid": list(wl.grid), "block": list(wl.block), "tokens": wl.L,
+                   "threshold": wl.threshold, "keep_ratio": wl.keep_ratio, "states": args.states, "layout": "block_major"},
+        "selected_block_fraction": int(b.lists.nnz.item()) / (b.shape.rows * b.shape.N), "ms_per_call": parts}))
+
+
 def measure(wl, steps, warmup, torch, B, traffic=True):
     """One workload: `warmup` untimed layers, then exactly `steps` layers (all five calls, forward +
     backward) in one event bracket, then the per-call breakdown.  Returns the result dict and the
@@ -422,6 +523,9 @@ def main():
     if over:
         wl = wl.replace(**over)
     torch.cuda.set_device(0)
+    if args.block:
+        block(args, wl, torch, B)
+        return
     out, ctx = measure(wl, args.steps, args.warmup, torch, B, traffic=not over)
     shp, dev, Q, K, V, dO, dQ, dK, dV, LSE = (ctx[k] for k in ("shp", "dev", "Q", "K", "V", "dO", "dQ", "dK", "dV", "LSE"))
     dense_flops, ms_step = ctx["dense_flops"], out["ms_per_step"]
