@@ -243,7 +243,8 @@ int bsa_dense_attn_bwd(const bsa_shape_t* shape, const void* Q, const void* K, c
  * as the norm gives them.  Arithmetic is fp32, each result is rounded once.  (A sum of squares beyond fp32, from
  * elements of 1e18 on, makes a row zero.)
  *   shape   B, H, T, Hs, Ws, d, dtype and layout; the block must divide the grid (1, 1, 1 will do for raster tensors),
- *           Bk and N are not limited here; B*L < 2^31.  A text or any other sequence: T = length, Hs = Ws = 1.
+ *           Bk and N are not limited here; B*L < 2^30, 2^29, 2^28 or 2^27 for d up to 32, 64, 128 or 256.  A text or any
+ *           other sequence: T = length, Hs = Ws = 1.
  *   rope    NULL: no rotation (table is not read either)
  *   table   device, bsa_rope_table_bytes(): for t, then h, then w: [extent][n_axis / 2][2] = cos, sin of every
  *           coordinate and pair.  bsa_rope_table() fills it; any other angles will do as well.
@@ -291,7 +292,8 @@ int bsa_qk_norm_rope_bwd(const bsa_shape_t* shape, const bsa_rope_t* rope, const
  * valid ones, O = softmax(sm_scale Q K^T) V.  Query head h reads key/value head h / (H / Hkv).
  * State s of batch entry b is valid if s < kv_len[b] and kv_mask[b][s] is not 0.  What K and V hold at other states is
  * never used, be it NaN.  A batch entry without a valid state gives O = 0 and LSE = -inf and has no gradients.
- *   shape    1 <= Hkv, Hkv divides H; Lq, S >= 1; B * H * ceil(Lq / 32) * ceil(S / 32) < 2^30; d a multiple of 8, at most 256
+ *   shape    1 <= Hkv, Hkv divides H; Lq, S >= 1; B * H * ceil(Lq / 32) * ceil(S / 32) < 2^30; d a multiple of 8, at most 256;
+ *            B * Hkv * ceil(H / Hkv * Lq / 128) < 2^23 and for the backward B * Hkv * ceil(S / 64) < 2^23
  *   q, k, v, o   strides of Q, K, V, O
  *   kv_len   device [B] int32, taken as 0 below 0 and as S above S; NULL: S for all
  *   kv_mask  device [B][S] bytes; NULL: all 1
@@ -313,7 +315,7 @@ int bsa_cross_attn_fwd(const bsa_cross_shape_t* shape, const void* Q, const void
 /*
  * Its backward.  dK and dV are sums over the query heads that share them, zero at states that are not valid; every
  * element of dQ, dK and dV is written.  delta = <dO, O> uses the O the caller passes (bf16, d <= 128: batch entries with
- * at most 128 states have it from the probabilities instead, the same number without the rounding of O).
+ * at most 128 states may have it from the probabilities instead, the same number without the rounding of O).
  *   O, LSE   the forward's outputs
  *   grads    host, strides of dO, dQ, dK, dV, in this order; NULL: those of O, Q, K, V
  *   K and V that repeat (stride 0) have a gradient for every repetition, whose sum is the caller's.

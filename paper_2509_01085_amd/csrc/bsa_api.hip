@@ -339,6 +339,7 @@ static int rope_args(const bsa_shape_t* shape, const bsa_rope_t* rope, const flo
   int rc = make_token_geom(shape, g);
   if (rc) return rc;
   if ((rc = rope_of(*g, rope, a)) != BSA_OK) return rc;
+  if (!rope_fits(*g)) return BSA_ERR_SHAPE;
   if (a->nt + a->nh + a->nw && !table) return BSA_ERR_NULL;
   if (!(eps > 0.f) || !std::isfinite(eps)) return BSA_ERR_RANGE;
   a->table = table;
@@ -356,6 +357,7 @@ static int cross_args(const bsa_cross_shape_t* s, CrossArgs* a) {
   // tiles of 32 queries by 32 keys, heads and batch: the kernels count them in 32 bits
   const int64_t tiles = (int64_t)((s->Lq + 31) / 32) * ((s->S + 31) / 32), heads = (int64_t)s->B * s->H;
   if (heads > 0x3fffffffLL / ((s->Lq + 31) / 32 + (s->S + 31) / 32) || tiles > 0x3fffffffLL / heads) return BSA_ERR_SHAPE;
+  if ((((int64_t)G * s->Lq + 127) / 128) * s->B * s->Hkv >= 1 << 23) return BSA_ERR_SHAPE;  // units: a launch has fewer than 2^32 threads
   a->B = s->B; a->H = s->H; a->Hkv = s->Hkv; a->G = G; a->Lq = s->Lq; a->M = G * s->Lq; a->S = s->S; a->d = s->d; a->dtype = s->dtype;
   return BSA_OK;
 }
@@ -491,6 +493,7 @@ int bsa_cross_attn_bwd(const bsa_cross_shape_t* shape, const void* Q, const void
   if (!(sm_scale > 0.f) || !std::isfinite(sm_scale)) return BSA_ERR_RANGE;
   for (const void* p : {Q, K, V, O, dO, (const void*)dQ, (const void*)dK, (const void*)dV})
     if (!aligned16(p)) return BSA_ERR_STRIDE;
+  if ((int64_t)((a.S + 63) / 64) * a.B * a.Hkv >= 1 << 23) return BSA_ERR_SHAPE;
   if ((rc = cross_strides(shape, &a, true)) != BSA_OK) return rc;
   a.go = grads ? grads[0] : shape->o;
   a.gq = grads ? grads[1] : shape->q;

@@ -175,6 +175,7 @@ struct RopeArgs {
 int launch_rope_table(const Geom& g, const RopeArgs& a, double theta, const double origin[3], float* table, hipStream_t st);
 int launch_rope_fwd(const Geom& g, int dtype, const RopeArgs& a, hipStream_t st);
 int launch_rope_bwd(const Geom& g, int dtype, const RopeArgs& a, hipStream_t st);
+bool rope_fits(const Geom& g);
 size_t rope_bwd_workspace(const Geom& g);
 
 // ---- bsa_cross_attn_* ----

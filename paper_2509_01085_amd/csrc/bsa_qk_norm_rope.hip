@@ -343,6 +343,8 @@ static int head_split(int64_t groups, int H) {
 
 static int lanes_of(int d) { return d <= 32 ? 4 : d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
+bool rope_fits(const Geom& g) { return (int64_t)g.B * g.L * lanes_of(g.d) < 0xffffff00LL; }  // a launch has fewer than 2^32 threads
+
 static dim3 bwd_grid(const Geom& g, int* heads) {
   const int rpw = 64 / lanes_of(g.d);
   const int64_t groups = ((int64_t)g.B * g.L + 4 * rpw - 1) / (4 * rpw);

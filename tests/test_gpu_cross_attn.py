@@ -249,3 +249,59 @@ def test_replayed_and_on_other_streams(name):
             step()
         side.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), f"stream {k}"
+
+
+@pytest.mark.parametrize("dtype", (H16, F))
+@pytest.mark.parametrize("Lq,S", ((1, 900), (40, 100), (300, 300)))
+def test_a_mask_that_leaves_nothing_of_an_entry_or_of_a_tile(Lq, S, dtype):
+    s = B.CrossShape(4, 4, 2, Lq, S, 64, dtype)
+    Q, K, V, dO, _, _ = tensors(dict(shape=s, lens=None, mask=False, lay="heads"), 31)
+    mask = torch.ones((4, S), dtype=torch.bool)
+    mask[0] = False          # nothing, and no length says so
+    mask[1, :70] = False     # not the first tile
+    mask[2, 1:] = False      # one state
+    lens = torch.tensor([S, S, S, 64], dtype=torch.int32)
+    mask[3, :64] = False     # nothing up to the length
+    ok = P.valid_states(4, S, lens, mask)
+    for t in (K, V):
+        t.masked_fill_(~ok.to(DEV)[:, None, :, None], NAN)
+    valid = dict(kv_len=lens.to(DEV), kv_mask=mask.to(DEV))
+    O, LSE = B.cross_attn_fwd(s, Q, K, V, **valid)
+    grads = B.cross_attn_bwd(s, Q, K, V, O, LSE, dO, **valid)
+    ref = reference(s, Q, K, V, ok, dO)
+    for n, t in zip(("O", "LSE", "dQ", "dK", "dV"), (O, LSE, *grads)):
+        P.check(n, t, ref[n], P.U32 if n == "LSE" else P.HALF[s.torch_dtype])
+    assert (O[0] == 0).all() and (O[3] == 0).all() and torch.isneginf(LSE[0]).all() and all((g[0] == 0).all() for g in grads)
+
+
+@pytest.mark.parametrize("dtype", (H16, F))
+@pytest.mark.parametrize("Lq,S,d", ((1, 500, 128), (35, 70, 64), (150, 33, 40), (5, 90, 256)))
+def test_more_entries_than_a_wavefront_has_lanes(Lq, S, d, dtype):
+    s = B.CrossShape(131, 2, 1, Lq, S, d, dtype)
+    gen = torch.Generator().manual_seed(S)
+    lens = torch.randint(0, S + 1, (131,), generator=gen)
+    lens[60:70] = 0
+    c = dict(shape=s, lens=lens.tolist(), mask=False, lay="heads")
+    Q, K, V, dO, ok, valid = tensors(c, S)
+    O, LSE = B.cross_attn_fwd(s, Q, K, V, **valid)
+    grads = B.cross_attn_bwd(s, Q, K, V, O, LSE, dO, **valid)
+    ref = reference(s, Q, K, V, ok, dO)
+    for n, t in zip(("O", "LSE", "dQ", "dK", "dV"), (O, LSE, *grads)):
+        P.check(n, t, ref[n], P.U32 if n == "LSE" else P.HALF[s.torch_dtype])
+
+
+@pytest.mark.parametrize("dtype", (H16, F))
+@pytest.mark.parametrize("B_,H,Lq,S,d", ((1, 4, 700, 200, 64), (2, 8, 500, 300, 256), (1, 3, 64, 1500, 128), (2, 2, 40, 700, 96)))
+def test_workspaces_of_the_size_that_is_asked_for_are_not_exceeded(B_, H, Lq, S, d, dtype):
+    s = B.CrossShape(B_, H, H, Lq, S, d, dtype)
+    for lens in (None, [S // 2 + 1] * B_):
+        Q, K, V, dO, ok, valid = tensors(dict(shape=s, lens=lens, mask=False, lay="heads"), 5)
+        wide = lambda n: torch.full((n + 4096,), 0x5a, dtype=torch.uint8, device=DEV)  # noqa: E731
+        nf, nb = B.cross_fwd_workspace_bytes(s), B.cross_bwd_workspace_bytes(s)
+        wf, wb = wide(nf), wide(nb)
+        O, LSE = B.cross_attn_fwd(s, Q, K, V, workspace=wf[:nf], **valid)
+        grads = B.cross_attn_bwd(s, Q, K, V, O, LSE, dO, workspace=wb[:nb], **valid)
+        assert (wf[nf:] == 0x5a).all() and (wb[nb:] == 0x5a).all()
+        ref = reference(s, Q, K, V, ok, dO)
+        for n, t in zip(("O", "dQ", "dK", "dV"), (O, *grads)):
+            P.check(n, t, ref[n], P.HALF[s.torch_dtype])

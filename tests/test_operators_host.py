@@ -172,3 +172,12 @@ def test_plain_cross_gradient_against_differences():
     want = (f(*(t + h * x for t, x in zip((Q, K, V), v))) - f(*(t - h * x for t, x in zip((Q, K, V), v)))) / (2 * h)
     got = sum(float((out[n][0] * x).sum()) for n, x in zip(("dQ", "dK", "dV"), v))
     assert abs(got - want) < 1e-7 * (1 + abs(want))
+
+
+def test_more_work_than_a_launch_takes_is_refused():
+    for d, most in ((32, 30), (64, 29), (128, 28), (256, 27)):
+        wide = B.Shape(1, 1, 1 << most, 1, 1, 1, 1, 1, d, B.BF16)
+        assert fwd(wide, rope=None, xs=(0, d, d)) == -2 and bwd(wide, rope=None, xs=(0, d, d), dxs=(0, d, d)) == -2, d
+    rows, keys = B.CrossShape(1, 1, 1, 1 << 30, 1, 8, B.BF16), B.CrossShape(1, 1, 1, 1, 1 << 29, 8, B.BF16)
+    assert cfwd(rows) == -2 and cbwd(rows) == -2 and cbwd(keys) == -2
+    assert B.cross_fwd_workspace_bytes(rows) == 0 and B.cross_fwd_workspace_bytes(keys) > 0
