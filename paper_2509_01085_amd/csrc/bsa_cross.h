@@ -101,6 +101,7 @@ struct TileView {
   // fp32: a value is one product's operand, and a product takes no longer than a value from LDS.  They run eight ahead of the products,
   // neighbours of which add to different accumulators.  (Row r has its chunks at c ^ (8 grp | r % 8): the address of row
   // 16 h + 8 a + 4 grp + e is that of 8 a + 4 grp + e and a constant, and a channel tile an exclusive or of bit 7 and a constant.)
+  // With the reads where the compiler puts them, one ahead of each product, dK and dV of 2,520 queries took 172 us instead of 127.
   __device__ inline void gather(f32x16 (&acc)[DP / 32], const uint8_t* tile, int row0, const f32x16& x) const {
     constexpr int DT = DP / 32;
     if constexpr (sizeof(T) == 2) {

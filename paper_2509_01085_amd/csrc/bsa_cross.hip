@@ -4,6 +4,19 @@
 // The G query heads that share keys are one matrix of M = G Lq rows, so shared heads cost nothing in the forward and dQ and
 // their gradients come out summed.  A workgroup has four wavefronts of 32 rows (forward, dQ) or 32 keys (dK, dV); the other
 // side's tiles stream through LDS in a ring of two, one barrier a tile.
+//
+//   S = Q K^T, P = exp(sm_scale S - LSE), O = P V;  dP = dO V^T, delta = <dO, O>, dS = P (dP - delta),
+//   dQ = sm_scale dS K, dK = sm_scale dS^T Q, dV = P^T dO
+//
+// Softmax statistics, sums and accumulators are fp32.  bf16: P and dS are rounded once on their way into a product, as its operands are
+// bf16; that and the result's own rounding are what the results are off by (O 2.2e-3 rms, gradients 2.4e-3 to 2.6e-3).
+//
+// What bounds them, and what they measured (512 states, 33,280 queries, 12 heads, d = 128, bf16): the forward took 131 us (105 GFLOP,
+// 0.80 PFLOP/s; a library product of 8192^3 reaches 1.4), dQ 190 (157 GFLOP, 0.83), dK and dV (bsa_cross_dkv.hip) 199 and 7 (209 GFLOP, 1.01).
+// About 30 us of the forward are the first tiles, the rows and the results, 204 MB; a further state costs 0.2 us, 1.06 PFLOP/s, where LDS reads
+// (42 us), matrix cores (42) and vector instructions (58) of two wavefronts a SIMD are in each other's way.  One query a head and
+// 20,000 states, 8 entries: 80 us, the bytes at the rate of a copy 84, and 14 to join the shares.  fp32: 118 TFLOP/s of the 154 that a
+// library product reaches (1,200 queries, 2,000 states, 48 heads: 501, 835 and 973 us).
 #include <algorithm>
 
 #include "bsa_cross.h"
@@ -783,8 +796,9 @@ static int padded_d(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // Forward and dQ: two workgroups a CU where registers and LDS allow it.  Shares where whole units would leave slots without work for
 // the time of `worth` tiles, which is what shares cost: the reckoning, the second launch, and at d = 128 a loop with fewer registers.
 // bf16: about 14 us, a tile takes 1.2.  fp32: 10 to 30 us, a tile 3 to 6, and one workgroup keeps a CU's matrix cores as busy as two, so
-// the CUs are counted, and shares taken only where half of them would have no unit.  4 heads of 64 channels, 700 queries, 200 states in fp32: 59 us whole, 31 in shares; 12 of 128, 2,520 queries, 333
-// states (240 units): 193 and 257; 48 of 1,200 queries, 2,000 states (480 units): 1,630 and 2,070.  Lengths are known on the device only and do not count here: shares for a batch of four of any length
+// the CUs are counted, and shares taken only where half of them would have no unit.  4 heads of 64 channels, 700 queries, 200 states
+// in fp32: 59 us whole, 36 in shares; 12 of 128, 2,520 queries, 333 states (240 units): 193 and 257; 48 of 1,200 queries, 2,000 states
+// (480 units): 1,630 and 2,070.  Lengths are known on the device only and do not count here: shares for a batch of four of any length
 // up to 2,000 (bf16, 480 units) took 204 us, whole units 128.
 static Deal rows_deal(const CrossArgs& a) {
   const bool f32 = a.dtype == BSA_F32;
