@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from math import sqrt
 from typing import Optional
@@ -50,6 +51,9 @@ class RopeStruct(C.Structure):
 class CrossStruct(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("B", "H", "Hkv", "Lq", "S", "d", "dtype")] + [(n, StridesStruct) for n in "qkvo"]
 
+
+# the same from one pack: field by field they take longer to fill than a small call to launch
+_CROSS, _FOUR, _FOUR_STRIDES = struct.Struct("7i4x12q"), struct.Struct("12q"), StridesStruct * 4
 
 _lib = None
 
@@ -358,15 +362,16 @@ class CrossShape:
 
     def c(self, Q=None, K=None, V=None, O=None) -> CrossStruct:
         """With the strides of the given [B, heads, tokens, d] tensors (contiguous ones where there is none)."""
-        return CrossStruct(self.B, self.H, self.Hkv, self.Lq, self.S, self.d, self.dtype,
-                           *(_strides(t, 2, 1) if t is not None else StridesStruct(h * n * self.d, self.d, n * self.d)
-                             for t, h, n in ((Q, self.H, self.Lq), (K, self.Hkv, self.S), (V, self.Hkv, self.S), (O, self.H, self.Lq))))
+        d, own = self.d, []
+        for t, h, n in ((Q, self.H, self.Lq), (K, self.Hkv, self.S), (V, self.Hkv, self.S), (O, self.H, self.Lq)):
+            own += (h * n * d, d, n * d) if t is None else _strides(t)
+        return CrossStruct.from_buffer_copy(_CROSS.pack(self.B, self.H, self.Hkv, self.Lq, self.S, d, self.dtype, *own))
 
 
-def _strides(t: torch.Tensor, l: int, h: int) -> StridesStruct:
-    """Of a tensor whose dimensions are batch, channels last and tokens and heads at l and h."""
-    s = t.stride()
-    return StridesStruct(s[0], s[l], s[h])
+def _strides(t: torch.Tensor):
+    """Batch, tokens and heads of a [B, heads, tokens, d] tensor."""
+    b, h, l, _ = t.stride()  # noqa: E741
+    return b, l, h
 
 
 def _device(t: torch.Tensor) -> torch.device:
@@ -377,11 +382,16 @@ def _device(t: torch.Tensor) -> torch.device:
     return device
 
 
+def _stream_of(device: torch.device) -> int:
+    """Its current stream, without the object around it."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _take(t: Optional[torch.Tensor], name: str, size, dtype, device, dense: bool = False) -> Optional[int]:
     """The address of a tensor of that size, type and device, its last dimension (dense: all of it) contiguous; None for None."""
     if t is None:
         return None
-    if t.shape != size or t.dtype != dtype or t.device != device:
+    if t.shape != size or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name} must be {tuple(size)} {dtype} on {device}, not {tuple(t.shape)} {t.dtype} on {t.device}")
     if not t.is_contiguous() and (dense or t.stride(-1) != 1 and t.shape[-1] > 1):
         raise ValueError(f"{name} must be contiguous" if dense else f"{name}: the channels of a head must be adjacent")
@@ -421,13 +431,16 @@ def _rope_table_ptr(shape, rope, table: Optional[torch.Tensor], device) -> Optio
 
 def _same_strides(tensors, names):
     """The common strides of the [B, L, H, d] tensors that are there (an extent of 1 has none)."""
-    there = [t for t in tensors if t is not None]
-    first = there[0]
-    strides = first.stride()
-    for t in there[1:]:
-        if t.stride() != strides and any(a != b and n > 1 for a, b, n in zip(t.stride(), strides, first.shape)):
+    first = None
+    for t in tensors:
+        if t is None:
+            continue
+        strides = t.stride()
+        if first is None:
+            first, size = strides, t.shape
+        elif strides != first and any(a != b and n > 1 for a, b, n in zip(strides, first, size)):
             raise ValueError(f"{names} must have the same strides")
-    return C.byref(_strides(first, 1, 2))
+    return C.byref(StridesStruct(*first[:3]))
 
 
 def qk_norm_rope_fwd(shape: Shape, rope: Optional[Rope], table: Optional[torch.Tensor], Xq=None, Xk=None, Xv=None,
@@ -444,7 +457,7 @@ def qk_norm_rope_fwd(shape: Shape, rope: Optional[Rope], table: Optional[torch.T
     outs = [_take(y, n, size_out, dt, dev, True) for y, n in zip(Y, "QKV")]
     sp, rp = C.byref(shape.c()), C.byref(rope.c()) if rope is not None else None
     st = lib().bsa_qk_norm_rope_fwd(sp, rp, _rope_table_ptr(sp, rp, table, dev), *args,
-                                    _same_strides(X, "Xq, Xk and Xv"), *w, eps, *outs, _stream())
+                                    _same_strides(X, "Xq, Xk and Xv"), *w, eps, *outs, _stream_of(dev))
     _check(st, "bsa_qk_norm_rope_fwd")
     return tuple(Y)
 
@@ -474,7 +487,7 @@ def qk_norm_rope_bwd(shape: Shape, rope: Optional[Rope], table: Optional[torch.T
     st = lib().bsa_qk_norm_rope_bwd(sp, rp, _rope_table_ptr(sp, rp, table, dev), *xs,
                                     _same_strides(X, "Xq and Xk") if any(t is not None for t in X) else None, *w, eps, *ys, *outs,
                                     _same_strides(dX, "dXq, dXk and dXv"), *dws, _ptr(workspace),
-                                    workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+                                    workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream_of(dev))
     _check(st, "bsa_qk_norm_rope_bwd")
     return (*dX, *dw)
 
@@ -505,7 +518,7 @@ def cross_attn_fwd(shape: CrossShape, Q, K, V, kv_len: Optional[torch.Tensor] = 
     c = shape.c(Q, K, V, O)
     workspace = _scratch(workspace, lib().bsa_cross_attn_fwd_workspace_bytes(C.byref(c)), dev)
     st = lib().bsa_cross_attn_fwd(C.byref(c), *ins, *valid, 1.0 / sqrt(shape.d) if sm_scale is None else sm_scale, *outs, _ptr(workspace),
-                                  workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+                                  workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream_of(dev))
     _check(st, "bsa_cross_attn_fwd")
     return O, LSE
 
@@ -528,10 +541,10 @@ def cross_attn_bwd(shape: CrossShape, Q, K, V, O, LSE, dO, kv_len: Optional[torc
     valid = _valid(shape, kv_len, kv_mask, dev)
     outs = [_take(t, n, s, dt, dev) for t, n, s in ((dQ, "dQ", qs), (dK, "dK", ks), (dV, "dV", ks))]
     c = shape.c(Q, K, V, O)
-    grads = (StridesStruct * 4)(*(_strides(t, 2, 1) for t in (dO, dQ, dK, dV)))
+    grads = _FOUR_STRIDES.from_buffer_copy(_FOUR.pack(*_strides(dO), *_strides(dQ), *_strides(dK), *_strides(dV)))
     workspace = _scratch(workspace, lib().bsa_cross_attn_bwd_workspace_bytes(C.byref(c)), dev)
     st = lib().bsa_cross_attn_bwd(C.byref(c), *ins, *valid, 1.0 / sqrt(shape.d) if sm_scale is None else sm_scale, *outs, grads,
-                                  _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream())
+                                  _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream_of(dev))
     _check(st, "bsa_cross_attn_bwd")
     return dQ, dK, dV
 
