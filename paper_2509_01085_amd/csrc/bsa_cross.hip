@@ -15,7 +15,7 @@
 // 0.80 PFLOP/s; a library product of 8192^3 reaches 1.4), dQ 190 (157 GFLOP, 0.83), dK and dV (bsa_cross_dkv.hip) 199 and 7 (209 GFLOP, 1.01).
 // About 30 us of the forward are the first tiles, the rows and the results, 204 MB; a further state costs 0.2 us, 1.06 PFLOP/s, where LDS reads
 // (42 us), matrix cores (42) and vector instructions (58) of two wavefronts a SIMD are in each other's way.  One query a head and
-// 20,000 states, 8 entries: 80 us, the bytes at the rate of a copy 84, and 14 to join the shares.  fp32: 118 TFLOP/s of the 154 that a
+// 20,000 states, 8 entries: 80 us, the bytes at the rate of a copy 84, and 9 to join the shares.  fp32: 118 TFLOP/s of the 154 that a
 // library product reaches (1,200 queries, 2,000 states, 48 heads: 501, 835 and 973 us).
 #include <algorithm>
 
@@ -382,28 +382,30 @@ __global__ __launch_bounds__(kThreads, (a_cu<T, DP, ONE>())) void cross_fwd_kern
   }
 }
 
-// Sum over the parts of a unit of the 16 values that a wavefront's channel tile has at `at` (values before it), each part times its
-// weight: eight parts' loads in flight.
-template <int VALUES, typename F>
-__device__ inline f32x16 sum_parts(float* part, const Parts& ps, int at, int wave, int lane, F weight) {
+// The 16 values that a wavefront's channel tile has at `at` (values before it), of eight parts from s on (the last one again where there
+// are fewer): their loads are in flight together.
+template <int VALUES>
+__device__ inline void load_parts(float (&v)[8][16], float* part, const Parts& ps, int s, int at, int wave, int lane) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float* in = part_of<VALUES>(part, ps.slot(min(s + j, ps.n - 1)), wave, lane) + at * 64;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[j][r] = in[r * 64];
+  }
+}
+template <int VALUES>
+__device__ inline f32x16 sum_parts(float* part, const Parts& ps, int at, int wave, int lane) {
   f32x16 acc;
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0.f;
   for (int s = 0; s < ps.n; s += 8) {
-    float v[8][16], f[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float* in = part_of<VALUES>(part, ps.slot(min(s + j, ps.n - 1)), wave, lane) + at * 64;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) v[j][r] = in[r * 64];
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = weight(min(s + j, ps.n - 1));
+    float v[8][16];
+    load_parts<VALUES>(v, part, ps, s, at, wave, lane);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (s + j < ps.n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] = f[j] != 0.f ? __builtin_fmaf(v[j][r], f[j], acc[r]) : acc[r];  // (a part without a key holds nothing)
+        for (int r = 0; r < 16; ++r) acc[r] += v[j][r];
   }
   return acc;
 }
@@ -420,39 +422,41 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_fwd_combine_kernel(CrossArgs,
   if (!u.any) return;
   const Parts ps(a, dl, lane, b, unit);
   if (ps.n == 0) return;
-  auto top_of = [&](int s) { return part_of<VALUES>(part, ps.slot(s), wave, lane)[DT * 16 * 64]; };
-  auto sum_of = [&](int s) { return part_of<VALUES>(part, ps.slot(s), wave, lane)[(DT * 16 + 1) * 64]; };
+  // one pass: what was summed is brought to the maximum of every further eight parts
   float m = kLowest, l = 0.f;
   bool any = false;
+  f32x16 o[1];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) o[0][r] = 0.f;
   for (int s = 0; s < ps.n; s += 8) {
-    float ms[8], ls[8];
+    float v[8][16], ms[8], ls[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      ms[j] = top_of(min(s + j, ps.n - 1));
-      ls[j] = sum_of(min(s + j, ps.n - 1));
+      const float* in = part_of<VALUES>(part, ps.slot(min(s + j, ps.n - 1)), wave, lane) + DT * 16 * 64;
+      ms[j] = in[0];
+      ls[j] = in[64];
     }
+    load_parts<VALUES>(v, part, ps, s, dt * 16, wave, lane);
+    float top = m;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {  // (the last part again and again changes nothing: sums are taken below)
+    for (int j = 0; j < 8; ++j) {  // (the last part again changes no maximum)
       any |= ls[j] != -1.f;
-      m = fmaxf(m, ls[j] == -1.f ? kLowest : ms[j]);
+      top = fmaxf(top, ls[j] == -1.f ? kLowest : ms[j]);
     }
-  }
-  auto weight = [&](int s) {
-    const float ms = top_of(s), ls = sum_of(s);
-    return ls == -1.f ? 0.f : __builtin_amdgcn_exp2f(ms - m);
-  };
-  for (int s = 0; s < ps.n; s += 8) {
-    float ms[8], ls[8];
+    const float was = __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    l *= was;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[0][r] *= was;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      ms[j] = top_of(min(s + j, ps.n - 1));
-      ls[j] = sum_of(min(s + j, ps.n - 1));
-    }
+      if (s + j >= ps.n || ls[j] == -1.f) continue;  // (a part without a key holds nothing)
+      const float f = __builtin_amdgcn_exp2f(ms[j] - m);
+      l = __builtin_fmaf(ls[j], f, l);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (s + j < ps.n && ls[j] != -1.f) l = __builtin_fmaf(ls[j], __builtin_amdgcn_exp2f(ms[j] - m), l);
+      for (int r = 0; r < 16; ++r) o[0][r] = __builtin_fmaf(v[j][r], f, o[0][r]);
+    }
   }
-  const f32x16 o[1] = {sum_parts<VALUES>(part, ps, dt * 16, wave, lane, weight)};
   store_column<T, 1>(static_cast<T*>(a.O_out) + u.offset(a, a.o) + 32 * dt, o, any ? 1.f / l : 0.f, a.d - 32 * dt, grp, u.live);
   if (dt == 0) put_lse(a, u, m, l, any, grp);
 }
@@ -648,7 +652,7 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_dq_combine_kernel(CrossArgs, 
   if (!u.any) return;
   const Parts ps(a, dl, lane, b, unit);
   if (ps.n == 0) return;
-  const f32x16 dq[1] = {sum_parts<DT * 16>(part, ps, dt * 16, wave, lane, [](int) { return 1.f; })};
+  const f32x16 dq[1] = {sum_parts<DT * 16>(part, ps, dt * 16, wave, lane)};
   store_column<T, 1>(static_cast<T*>(a.dQ) + u.offset(a, a.gq) + 32 * dt, dq, a.sm_scale, a.d - 32 * dt, lane >> 5, u.live);
 }
 
@@ -784,7 +788,7 @@ __global__ __launch_bounds__(2 * DP, 1) void cross_dkv_combine_kernel(CrossArgs,
   const KeyUnit u(a, b, unit, wave, lane);
   const Parts ps(a, dl, lane, b, unit);
   if (ps.n == 0) return;
-  const f32x16 acc[1] = {sum_parts<DT * 32>(part, ps, (is_v * DT + dt) * 16, wave, lane, [](int) { return 1.f; })};
+  const f32x16 acc[1] = {sum_parts<DT * 32>(part, ps, (is_v * DT + dt) * 16, wave, lane)};
   const auto& st = is_v ? a.gv : a.gk;
   store_column<T, 1>(static_cast<T*>(is_v ? a.dV : a.dK) + u.b * st.b + u.hk * st.h + u.key * st.l + 32 * dt, acc, is_v ? 1.f : a.sm_scale,
                      a.d - 32 * dt, lane >> 5, u.there);
