@@ -175,9 +175,14 @@ struct Walk {
     if (!asked && pc.t0 < pc.t1) bits = ring.request(a, Keys(a, pc.b).bits(pc.t0 * KT, KT, ring.lane), pc.b, hk, pc.t0, place);
     asked = true;
   }
-  // Both tiles of a piece of one or two, now.
+  // Both tiles of a piece of one or two, now.  BEHIND: pieces may have come before it, whose last tile lies where the second one goes, and
+  // wavefronts may be at its products still: the last barrier was ahead of them.
+  template <bool BEHIND>
   __device__ __forceinline__ void both(Args& a, const Piece& pc, int hk) {
-    if (pc.t1 == 2) second = ring.request(a, Keys(a, pc.b).bits(KT, KT, ring.lane), pc.b, hk, 1, place ^ 1);
+    if (pc.t1 == 2) {
+      if constexpr (BEHIND) raw_barrier();
+      second = ring.request(a, Keys(a, pc.b).bits(KT, KT, ring.lane), pc.b, hk, 1, place ^ 1);
+    }
     here = true;
     wait_vm<0>();
     raw_barrier();
@@ -594,7 +599,7 @@ __global__ __launch_bounds__(kThreads, (a_cu<T, DP, false>())) void cross_dq_ker
       Fragments<DP> fg(uniform_lds(smem) + walk.place * 2 * Ring::TILE, lane);
       auto on = [&](int place) { fg.move(place ? -2 * Ring::TILE : 2 * Ring::TILE); };
       if (few) {
-        walk.both(a, pc, u.hk);
+        walk.template both<!ONE>(a, pc, u.hk);
         if (u.any) {
 #pragma unroll 1
           for (int t = 0; t < pc.t1; ++t) {
