@@ -55,8 +55,9 @@ enum bsa_status {
   BSA_ERR_LAUNCH = -6,      /* the HIP runtime reported a launch error */
   BSA_ERR_WORKSPACE = -7,   /* workspace NULL or smaller than the *_workspace_bytes() figure */
   BSA_ERR_STATIC_LIMIT = -8, /* bsa_select_kv_static: the shape needs more than BSA_STATIC_SELECT_BYTES */
-  BSA_ERR_STRIDE = -9       /* bsa_qk_norm_rope_*, bsa_cross_attn_*: a stride or address that is no multiple of 16
-                               bytes, a negative or huge stride, or an output whose elements would overlap */
+  BSA_ERR_STRIDE = -9       /* bsa_qk_norm_rope_*, bsa_cross_attn_*: a stride or an address of a tensor or workspace that is no
+                               multiple of 16 bytes, a rotation table's that is none of 8, a negative or huge stride, or an
+                               output whose elements would overlap */
 };
 
 /* Strides of a tensor with a batch, a token and a head index, in elements; the channels of a head are adjacent.
@@ -246,7 +247,7 @@ int bsa_dense_attn_bwd(const bsa_shape_t* shape, const void* Q, const void* K, c
  *           Bk and N are not limited here; B*L < 2^30, 2^29, 2^28 or 2^27 for d up to 32, 64, 128 or 256.  A text or any
  *           other sequence: T = length, Hs = Ws = 1.
  *   rope    NULL: no rotation (table is not read either)
- *   table   device, bsa_rope_table_bytes(): for t, then h, then w: [extent][n_axis / 2][2] = cos, sin of every
+ *   table   device, 8-byte aligned, bsa_rope_table_bytes(): for t, then h, then w: [extent][n_axis / 2][2] = cos, sin of every
  *           coordinate and pair.  bsa_rope_table() fills it; any other angles will do as well.
  *   Xq, Xk, Xv   in  [B, L, H, d] shape.dtype, tokens in raster order, all of strides x: separate tensors or slices of a
  *                    packed projection
@@ -277,7 +278,7 @@ int bsa_qk_norm_rope_fwd(const bsa_shape_t* shape, const bsa_rope_t* rope, const
  *   dXq, dXk, dXv  out [B, L, H, d] of strides dx
  *   dwq, dwk       out [d] float, sums over batch, tokens and heads in a fixed order; NULL: not wanted
  * Xq, dQ and dXq come together or not at all, so do Xk, dK and dXk, and dV and dXv.
- *   workspace      bsa_qk_norm_rope_bwd_workspace_bytes(shape) bytes of device scratch
+ *   workspace      bsa_qk_norm_rope_bwd_workspace_bytes(shape) bytes of device scratch, 16-byte aligned
  */
 size_t bsa_qk_norm_rope_bwd_workspace_bytes(const bsa_shape_t* shape);
 int bsa_qk_norm_rope_bwd(const bsa_shape_t* shape, const bsa_rope_t* rope, const float* table,
@@ -298,7 +299,7 @@ int bsa_qk_norm_rope_bwd(const bsa_shape_t* shape, const bsa_rope_t* rope, const
  *   kv_len   device [B] int32, taken as 0 below 0 and as S above S; NULL: S for all
  *   kv_mask  device [B][S] bytes; NULL: all 1
  *   LSE      out [B, H, Lq] contiguous float, natural-log sum-exp
- *   workspace  bsa_cross_attn_fwd_workspace_bytes(shape) bytes of device scratch (may be NULL when that is 0): partial
+ *   workspace  bsa_cross_attn_fwd_workspace_bytes(shape) bytes of device scratch, 16-byte aligned (may be NULL when that is 0): partial
  *              results where few query rows have their keys split over several workgroups
  */
 typedef struct bsa_cross_shape {
@@ -319,6 +320,7 @@ int bsa_cross_attn_fwd(const bsa_cross_shape_t* shape, const void* Q, const void
  *   O, LSE   the forward's outputs
  *   grads    host, strides of dO, dQ, dK, dV, in this order; NULL: those of O, Q, K, V
  *   K and V that repeat (stride 0) have a gradient for every repetition, whose sum is the caller's.
+ *   workspace  bsa_cross_attn_bwd_workspace_bytes(shape) bytes of device scratch, 16-byte aligned
  */
 size_t bsa_cross_attn_bwd_workspace_bytes(const bsa_cross_shape_t* shape);
 int bsa_cross_attn_bwd(const bsa_cross_shape_t* shape, const void* Q, const void* K, const void* V,

@@ -82,7 +82,7 @@ const char* bsa_strerror(int status) {
     case BSA_ERR_LAUNCH: return "HIP launch error";
     case BSA_ERR_WORKSPACE: return "workspace missing or too small";
     case BSA_ERR_STATIC_LIMIT: return "shape needs more scratch than the library's built-in buffer holds (BSA_STATIC_SELECT_BYTES)";
-    case BSA_ERR_STRIDE: return "strides and addresses must be multiples of 16 bytes, strides in [0, 2^40), outputs without overlap";
+    case BSA_ERR_STRIDE: return "strides and addresses (workspaces too) must be multiples of 16 bytes, a rotation table's of 8, strides in [0, 2^40), outputs without overlap";
     default: return "unknown bsa status";
   }
 }
@@ -288,6 +288,14 @@ int bsa_dense_attn_bwd(const bsa_shape_t* shape, const void* Q, const void* K, c
 namespace bsa {
 
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+static bool aligned8(const void* p) { return ((uintptr_t)p & 7) == 0; }  // cosine and sine are one load
+
+// Partial results and row statistics move in 16 bytes.
+static int fit_workspace(const void* p, size_t bytes, size_t need) {
+  if (!need) return BSA_OK;
+  if (!p || bytes < need) return BSA_ERR_WORKSPACE;
+  return aligned16(p) ? BSA_OK : BSA_ERR_STRIDE;
+}
 
 // Multiples of 16 bytes in range; the stride of an extent of 1 becomes 0.
 static int fit_strides(bsa_strides_t* s, int64_t b, int64_t l, int64_t h, int dtype) {
@@ -340,7 +348,10 @@ static int rope_args(const bsa_shape_t* shape, const bsa_rope_t* rope, const flo
   if (rc) return rc;
   if ((rc = rope_of(*g, rope, a)) != BSA_OK) return rc;
   if (!rope_fits(*g)) return BSA_ERR_SHAPE;
-  if (a->nt + a->nh + a->nw && !table) return BSA_ERR_NULL;
+  if (a->nt + a->nh + a->nw) {
+    if (!table) return BSA_ERR_NULL;
+    if (!aligned8(table)) return BSA_ERR_STRIDE;
+  }
   if (!(eps > 0.f) || !std::isfinite(eps)) return BSA_ERR_RANGE;
   a->table = table;
   a->eps = eps;
@@ -390,6 +401,7 @@ int bsa_rope_table(const bsa_shape_t* shape, const bsa_rope_t* rope, double thet
   if (rc) return rc;
   if ((rc = rope_of(g, rope, &a)) != BSA_OK) return rc;
   if (!rope || !table) return BSA_ERR_NULL;
+  if (!aligned8(table)) return BSA_ERR_STRIDE;
   if (!(theta > 0.0) || !std::isfinite(theta)) return BSA_ERR_RANGE;
   const double origin[3] = {(double)t0, (double)h0, (double)w0};
   return launch_rope_table(g, a, theta, origin, table, (hipStream_t)stream);
@@ -449,7 +461,7 @@ int bsa_qk_norm_rope_bwd(const bsa_shape_t* shape, const bsa_rope_t* rope, const
   }
   a.dx = *dx;
   if ((rc = fit_out_strides(&a.dx, g.B, g.L, g.H, g.d, shape->dtype)) != BSA_OK) return rc;
-  if (!workspace || workspace_bytes < rope_bwd_workspace(g)) return BSA_ERR_WORKSPACE;
+  if ((rc = fit_workspace(workspace, workspace_bytes, rope_bwd_workspace(g))) != BSA_OK) return rc;
   a.w[0] = wq; a.w[1] = wk;
   a.part = static_cast<float*>(workspace);
   return launch_rope_bwd(g, shape->dtype, a, (hipStream_t)stream);
@@ -470,8 +482,7 @@ int bsa_cross_attn_fwd(const bsa_cross_shape_t* shape, const void* Q, const void
   if (!(sm_scale > 0.f) || !std::isfinite(sm_scale)) return BSA_ERR_RANGE;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return BSA_ERR_STRIDE;
   if ((rc = cross_strides(shape, &a, false)) != BSA_OK) return rc;
-  const size_t need = cross_fwd_workspace(a);
-  if (need && (!workspace || workspace_bytes < need)) return BSA_ERR_WORKSPACE;
+  if ((rc = fit_workspace(workspace, workspace_bytes, cross_fwd_workspace(a))) != BSA_OK) return rc;
   a.Q = Q; a.K = K; a.V = V; a.kv_len = kv_len; a.kv_mask = kv_mask; a.sm_scale = sm_scale;
   a.O_out = O; a.LSE_out = LSE; a.ws = workspace; a.ws_bytes = workspace ? workspace_bytes : 0;
   return launch_cross_fwd(a, (hipStream_t)stream);
@@ -503,7 +514,7 @@ int bsa_cross_attn_bwd(const bsa_cross_shape_t* shape, const void* Q, const void
   if ((rc = fit_strides(&a.go, a.B, a.Lq, a.H, t)) || (rc = fit_out_strides(&a.gq, a.B, a.Lq, a.H, a.d, t)) ||
       (rc = fit_out_strides(&a.gk, a.B, a.S, a.Hkv, a.d, t)) || (rc = fit_out_strides(&a.gv, a.B, a.S, a.Hkv, a.d, t)))
     return rc;
-  if (!workspace || workspace_bytes < cross_bwd_workspace(a)) return BSA_ERR_WORKSPACE;
+  if ((rc = fit_workspace(workspace, workspace_bytes, cross_bwd_workspace(a))) != BSA_OK) return rc;
   a.Q = Q; a.K = K; a.V = V; a.O = O; a.LSE_in = LSE; a.dO = dO; a.kv_len = kv_len; a.kv_mask = kv_mask;
   a.sm_scale = sm_scale; a.dQ = dQ; a.dK = dK; a.dV = dV; a.ws = workspace; a.ws_bytes = workspace_bytes;
   return launch_cross_bwd(a, (hipStream_t)stream);
