@@ -202,13 +202,20 @@ struct Requests {
         dma16_raw(from, STEPS ? off : off + (channel(n) - channel(0)) * (int)sizeof(T), same(lds + n * NT * 16));
       }
   }
-  // The first `left` rows are there (offsets fit); the last of them stands in for the others, whose weights are zero.
+  // The first `left` rows are there (offsets fit).  The others' weights are zero: the last row stands in for them, or (ZEROS) zeros, so that
+  // an infinity of its own makes no NaN.  (Zeros written here: 492 of 512 states, 33,280 queries, 12 heads 141 us, requested from a chunk of zeros
+  // 142, the last row 139.)
+  template <bool ZEROS>
   __device__ __forceinline__ void cut(uint8_t* tile, const T* base, int64_t stride, int left) const {
     const uint64_t sbase = uniform64(base);
     const uint32_t lds = uniform_lds(tile + (tid >> 6) * 1024), step = (uint32_t)(stride * (int64_t)sizeof(T));
 #pragma unroll
     for (int n = 0; n < N; ++n)
-      if (channel(n) < d) dma16_raw(uniform64((const void*)sbase), min(row(n), left - 1) * step + channel(n) * (uint32_t)sizeof(T), same(lds + n * NT * 16));
+      if (channel(n) < d) {
+        if (!ZEROS || row(n) < left)
+          dma16_raw(uniform64((const void*)sbase), min(row(n), left - 1) * step + channel(n) * (uint32_t)sizeof(T), same(lds + n * NT * 16));
+        else *reinterpret_cast<u32x4*>(tile + (n * NT + tid) * 16) = u32x4{0, 0, 0, 0};
+      }
   }
   // Rows whose bit in `there` is not set arrive as zeros.
   __device__ __forceinline__ void some(uint8_t* tile, const T* base, int64_t stride, uint64_t there) const {
@@ -220,9 +227,10 @@ struct Requests {
       dma16(src, tile + (n * NT + wave * 64) * 16);
     }
   }
-  __device__ __forceinline__ void operator()(uint8_t* tile, const T* base, int64_t stride, uint64_t there, bool near) const {
+  template <bool ZEROS = false>
+  __device__ __forceinline__ void load(uint8_t* tile, const T* base, int64_t stride, uint64_t there, bool near) const {
     if (near && there == (ROWS == 64 ? ~0ull : (1ull << ROWS) - 1)) whole(tile, base);
-    else if (near && there && !(there & (there + 1))) cut(tile, base, stride, __popcll(there));
+    else if (near && there && !(there & (there + 1))) cut<ZEROS>(tile, base, stride, __popcll(there));
     else some(tile, base, stride, there);
   }
 };

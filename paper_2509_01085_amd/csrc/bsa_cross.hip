@@ -133,8 +133,9 @@ __device__ inline void finish_row(Args& a, const RowUnit& u, const f32x16 (&acc)
   put_lse(a, u, m, l, any, grp);
 }
 
-// The K and V tiles of a piece on their way through the ring of two.
-template <typename T, int DP>
+// The K and V tiles of a piece on their way through the ring of two.  SUMS: V's rows are summed (forward), so that one that is not there must
+// not show; elsewhere it stands beside K's, whose product with it has no weight.
+template <typename T, int DP, bool SUMS>
 struct KvRing {
   static constexpr int KT = key_tile<T, DP>(), TILE = KT * DP * (int)sizeof(T);
   uint8_t* smem;
@@ -151,8 +152,8 @@ struct KvRing {
     const T* K = static_cast<const T*>(a.K) + b * a.k.b + hk * a.k.h + (int64_t)t * KT * a.k.l;
     const T* V = static_cast<const T*>(a.V) + b * a.v.b + hk * a.v.h + (int64_t)t * KT * a.v.l;
     uint8_t* at = smem + place * 2 * TILE;
-    rk(at, K, a.k.l, there, a.near);
-    rv(at + TILE, V, a.v.l, there, a.near);
+    rk.load(at, K, a.k.l, there, a.near);
+    rv.template load<SUMS>(at + TILE, V, a.v.l, there, a.near);
     return there;
   }
   static constexpr uint64_t ALL = KT == 64 ? ~0ull : (1ull << KT) - 1;
@@ -160,16 +161,16 @@ struct KvRing {
 
 // A workgroup's walk over its pieces and their tiles.  While a tile is multiplied the next one is on its way, be it this piece's or the
 // next one's: `place` is the multiplied tile's, the other one the requested tile's.
-template <typename T, int DP>
+template <typename T, int DP, bool SUMS>
 struct Walk {
   static constexpr int KT = key_tile<T, DP>();
-  const KvRing<T, DP>& ring;
+  const KvRing<T, DP, SUMS>& ring;
   int place = 0;
   bool asked = false;  // the coming piece's first tile has been requested
   uint64_t bits = 0;   // its valid keys
   uint64_t second = 0; // those of the piece's second tile, if that is there already
   bool here = false;
-  __device__ inline explicit Walk(const KvRing<T, DP>& r) : ring(r) {}
+  __device__ inline explicit Walk(const KvRing<T, DP, SUMS>& r) : ring(r) {}
   // Requests a piece's first tile, unless that was done while the piece before it ended.
   __device__ __forceinline__ void ask(Args& a, const Piece& pc, int hk) {
     if (!asked && pc.t0 < pc.t1) bits = ring.request(a, Keys(a, pc.b).bits(pc.t0 * KT, KT, ring.lane), pc.b, hk, pc.t0, place);
@@ -311,12 +312,12 @@ __device__ inline void fwd_tile(Walked<D / 32>& w, const Fragments<D>& fg, const
 // ONE: a unit a workgroup (Deal::EACH), without what the walk over several pieces needs.
 template <typename T, int DP, bool ONE>
 __global__ __launch_bounds__(kThreads, (a_cu<T, DP, ONE>())) void cross_fwd_kernel(CrossArgs, Deal dl, float* part) {
-  using Ring = KvRing<T, DP>;
+  using Ring = KvRing<T, DP, true>;
   constexpr int KT = key_tile<T, DP>(), NK = KT / 32, DT = DP / 32;
   extern __shared__ __align__(16) uint8_t smem[];  // [2][K tile | V tile]
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Ring ring(smem, *kernel_args(), tid);
-  Walk<T, DP> walk(ring);
+  Walk<T, DP, true> walk(ring);
   Dealer<ONE> dealer(*kernel_args(), dl, tid & 63);
   Piece pc, nx;
   if (!dealer.next(pc)) return;
@@ -560,12 +561,12 @@ __device__ inline float delta_tile(const Fragments<D>& fg, const bf16x8* q, cons
 
 template <typename T, int DP, bool ONE>
 __global__ __launch_bounds__(kThreads, (a_cu<T, DP, false>())) void cross_dq_kernel(CrossArgs, Deal dl, float* stat, float* part) {
-  using Ring = KvRing<T, DP>;
+  using Ring = KvRing<T, DP, false>;
   constexpr int KT = key_tile<T, DP>(), NK = KT / 32, DT = DP / 32;
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Ring ring(smem, *kernel_args(), tid);
-  Walk<T, DP> walk(ring);
+  Walk<T, DP, false> walk(ring);
   Dealer<ONE> dealer(*kernel_args(), dl, tid & 63);
   Piece pc, nx;
   bool more = dealer.next(nx);
@@ -726,8 +727,8 @@ __device__ inline void dkv_walk(const Deal& dl, const float* stat, float* part) 
     uint8_t* at = smem + (t & 1) * STAGE;
     const T* Q = static_cast<const T*>(a.Q) + u.b * a.q.b + (int64_t)head * a.q.h + first * a.q.l;
     const T* G = static_cast<const T*>(a.dO) + u.b * a.go.b + (int64_t)head * a.go.h + first * a.go.l;
-    rq(at, Q, a.q.l, there, a.near);
-    rg(at + TILE, G, a.go.l, there, a.near);
+    rq.load(at, Q, a.q.l, there, a.near);
+    rg.load(at + TILE, G, a.go.l, there, a.near);
     if (tid < 16) dma16(stat + (((int64_t)u.b * a.H + head) * tiles + i) * 64 + 4 * tid, at + 2 * TILE);
   };
   if (t0 < t1) request(t0);
