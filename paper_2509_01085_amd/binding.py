@@ -468,15 +468,17 @@ def qk_norm_rope_bwd_workspace_bytes(shape: Shape) -> int:
 
 def qk_norm_rope_bwd(shape: Shape, rope: Optional[Rope], table: Optional[torch.Tensor], Xq=None, Xk=None, dQ=None, dK=None, dV=None,
                      wq=None, wk=None, eps: float = 1e-6, dXq=None, dXk=None, dXv=None, dwq=None, dwk=None,
-                     workspace: Optional[torch.Tensor] = None):
-    """Returns dXq, dXk, dXv ([B, L, H, d], contiguous where not given, then all of the same strides), dwq, dwk ([d] float)."""
+                     workspace: Optional[torch.Tensor] = None, weight_grads: bool = True):
+    """Returns dXq, dXk, dXv ([B, L, H, d], contiguous where not given, then all of the same strides), dwq, dwk ([d] float).
+    weight_grads=False: dwq and dwk only into memory that is given (None otherwise), and without either one launch less."""
     dY, X = (dQ, dK, dV), (Xq, Xk)
     if all(t is None for t in dY):
         raise ValueError("dQ, dK or dV must be given")
     dev, dt = _device(next(t for t in dY if t is not None)), shape.torch_dtype
     size_x, size_y = (shape.B, shape.L, shape.H, shape.d), (shape.B, shape.H, shape.L, shape.d)
     dX = [torch.empty(size_x, dtype=dt, device=dev) if y is not None and x is None else x for y, x in zip(dY, (dXq, dXk, dXv))]
-    dw = [torch.empty(shape.d, dtype=torch.float32, device=dev) if y is not None and t is None else t for y, t in zip(dY, (dwq, dwk))]
+    dw = [torch.empty(shape.d, dtype=torch.float32, device=dev) if weight_grads and y is not None and t is None else t
+          for y, t in zip(dY, (dwq, dwk))]
     xs = [_take(t, n, size_x, dt, dev) for t, n in zip(X, ("Xq", "Xk"))]
     w = [_take(t, n, (shape.d,), torch.float32, dev, True) for t, n in ((wq, "wq"), (wk, "wk"))]
     ys = [_take(t, n, size_y, dt, dev, True) for t, n in zip(dY, ("dQ", "dK", "dV"))]
