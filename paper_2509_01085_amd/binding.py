@@ -382,9 +382,14 @@ def _device(t: torch.Tensor) -> torch.device:
     return device
 
 
+# The current stream's handle without the object around it: 0.1 us instead of 2.6, of a call that takes 10.  No public name, so a torch
+# without it is served by the public one.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_of(device: torch.device) -> int:
-    """Its current stream, without the object around it."""
-    return torch._C._cuda_getCurrentRawStream(device.index)
+    """Its current stream."""
+    return _raw_stream(device.index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _take(t: Optional[torch.Tensor], name: str, size, dtype, device, dense: bool = False) -> Optional[int]:
