@@ -315,9 +315,12 @@ int bsa_cross_attn_fwd(const bsa_cross_shape_t* shape, const void* Q, const void
 
 /*
  * Its backward.  dK and dV are sums over the query heads that share them, zero at states that are not valid; every
- * element of dQ, dK and dV is written.  delta = <dO, O> uses the O the caller passes (bf16, d <= 128: batch entries with
- * at most 128 states may have it from the probabilities instead, the same number without the rounding of O).
- *   O, LSE   the forward's outputs
+ * element of dQ, dK and dV is written.
+ *   O, LSE   what bsa_cross_attn_fwd gave for the same Q, K, V, valid states and sm_scale, and nothing else: delta, the sum over a
+ *            row's states of P dP, is <dO, O> with the O passed, or (bf16, d <= 128, entries of at most 128 states) formed from
+ *            the probabilities, without the rounding of O.  The two are one number for that O alone; with O and LSE of a softmax
+ *            joined from several sets of states the gradients of one set would be wrong in the second case.
+ *   dO       an infinity makes the gradients that it goes into infinite or NaN
  *   grads    host, strides of dO, dQ, dK, dV, in this order; NULL: those of O, Q, K, V
  *   K and V that repeat (stride 0) have a gradient for every repetition, whose sum is the caller's.
  *   workspace  bsa_cross_attn_bwd_workspace_bytes(shape) bytes of device scratch, 16-byte aligned

@@ -539,7 +539,8 @@ def _valid(shape: CrossShape, kv_len, kv_mask, dev):
 
 def cross_attn_bwd(shape: CrossShape, Q, K, V, O, LSE, dO, kv_len: Optional[torch.Tensor] = None, kv_mask: Optional[torch.Tensor] = None,
                    sm_scale: Optional[float] = None, dQ=None, dK=None, dV=None, workspace: Optional[torch.Tensor] = None):
-    """dO, dQ, dK, dV may have strides of their own.  Of K and V that repeat (expanded), dK and dV hold every repetition's gradient."""
+    """O, LSE: cross_attn_fwd's for the same arguments, and no others.  dO, dQ, dK, dV may have strides of their own.  Of K and V that
+    repeat (expanded), dK and dV hold every repetition's gradient."""
     dev, dt = _device(Q), shape.torch_dtype
     dQ, dK, dV = (_like(t) if g is None else g for t, g in ((Q, dQ), (K, dK), (V, dV)))
     qs, ks = (shape.B, shape.H, shape.Lq, shape.d), (shape.B, shape.Hkv, shape.S, shape.d)

@@ -589,7 +589,7 @@ __global__ __launch_bounds__(kThreads, (a_cu<T, DP, false>())) void cross_dq_ker
     more = !ONE && dealer.next(nx);
     // A bf16 unit of no more than two tiles, which the ring holds: delta from the probabilities, a pass over both ahead of the
     // other.  With so few keys the rounding of O is what the gradients' error would mostly be (19 keys, d = 80: dQ 3.2e-3 off, rms),
-    // and O is not read.
+    // and O is not read.  (It has to be this softmax's: for another O, as of more states than these, the two are different numbers.)
     const bool few = sizeof(T) == 2 && DP <= 128 && pc.slot < 0 && pc.t1 > 0 && pc.t1 <= 2;
     float delta = few ? 0.f : pair_sum(gr.dot(static_cast<const T*>(a.O) + u.offset(a, a.o)));
     q.arrive();
