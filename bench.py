@@ -107,8 +107,8 @@ def parse():
                          "backward), one JSON line per length, at the paper's token counts from 23K to 153K")
     ap.add_argument("--block", action="store_true",
                     help="the attention part of a transformer block on the workload's shape instead: norm and rotation of a packed "
-                         "projection, sparse self-attention in block-major order, cross attention to --states encoder states, forward "
-                         "and backward; one JSON line with the time of every call")
+                         "projection (each head by itself), sparse self-attention in block-major order, cross attention to --states "
+                         "encoder states, forward and backward; one JSON line with the time of every call")
     ap.add_argument("--states", type=int, default=512, help="encoder states of --block")
     ap.add_argument("--calibration-copy-mib", type=int, default=0,
                     help="also run one plain elementwise copy of this many MiB (read + write that much each), "
@@ -287,7 +287,8 @@ class BlockAttention:
     """The attention part of a transformer block, forward and backward, on one GPU: the projection's queries, keys and values
     [B, L, 3, H, d] are normalised, rotated and brought to block-major [B, H, L, d]; sparse self-attention; cross attention of queries
     [B, L, H, d] of a second projection to the packed keys and values [B, states, 2, H, d] of an encoder.  The projections themselves are
-    the caller's.  Every buffer is allocated here, once."""
+    the caller's.  A workload's name gives the shape: the norm is one for each head, and Wan2.1, whose layer the benchmark's is, has its own
+    over the channels of all heads.  Every buffer is allocated here, once."""
 
     EPS = 1e-6
 

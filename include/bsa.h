@@ -237,7 +237,8 @@ int bsa_dense_attn_bwd(const bsa_shape_t* shape, const void* Q, const void* K, c
  * Per-head norm of queries and keys with the rotation by grid position in the same pass: what stands between a block's
  * projections and its attention.  For every token n = (t, h, w) and head
  *   Q = R(n) (wq * xq / sqrt(mean(xq^2) + eps)),  K likewise with xk and wk,  V = xv,
- * where x is a head's d channels of the projection's output and R(n) turns pairs of channels (a, b) by an angle,
+ * where x is a head's d channels of the projection's output, over which the mean runs too (a norm for each head: one over the
+ * channels of all heads together, as some models have it, is another operator), and R(n) turns pairs of channels (a, b) by an angle,
  *   (a, b) -> (a cos - b sin, a sin + b cos),  angle = position * theta^(-2i/n_axis).
  * Of the rope->dt + dh + dw rotated channels the first dt / 2 pairs turn with the token's t, the next dh / 2 with its h
  * and the last dw / 2 with its w (i counts an axis's own pairs, n_axis is dt, dh or dw); the channels behind them are left
