@@ -49,7 +49,8 @@ enum bsa_status {
   BSA_OK = 0,
   BSA_ERR_NULL = -1,        /* a required pointer is NULL */
   BSA_ERR_SHAPE = -2,       /* non-positive extent, block does not divide grid, unsupported d / Bk / N */
-  BSA_ERR_RANGE = -3,       /* threshold or keep ratio outside (0, 1], n_keep outside [1, Bk], sm_scale <= 0 */
+  BSA_ERR_RANGE = -3,       /* threshold or keep ratio outside (0, 1], n_keep outside [1, Bk], sm_scale <= 0, eps <= 0 or
+                               subnormal, theta <= 0, or any of them not finite */
   BSA_ERR_CAPACITY = -4,    /* index buffer smaller than the worst case rows*N */
   BSA_ERR_DTYPE = -5,       /* shape.dtype is neither BSA_F32 nor BSA_BF16 */
   BSA_ERR_LAUNCH = -6,      /* the HIP runtime reported a launch error */
@@ -270,7 +271,7 @@ int bsa_rope_table(const bsa_shape_t* shape, const bsa_rope_t* rope, double thet
                    float* table, void* stream);
 int bsa_qk_norm_rope_fwd(const bsa_shape_t* shape, const bsa_rope_t* rope, const float* table,
                          const void* Xq, const void* Xk, const void* Xv, const bsa_strides_t* x,
-                         const float* wq, const float* wk, float eps /* > 0 */,
+                         const float* wq, const float* wk, float eps /* > 0, normal: 2^-126 at least */,
                          void* Q, void* K, void* V, void* stream);
 
 /*

@@ -76,7 +76,7 @@ const char* bsa_strerror(int status) {
     case BSA_OK: return "ok";
     case BSA_ERR_NULL: return "a required pointer is NULL";
     case BSA_ERR_SHAPE: return "unsupported shape (extents must be positive, the block must divide the grid, d%8==0, d<=256, Bk<=256, N<=8192)";
-    case BSA_ERR_RANGE: return "threshold / keep ratio must lie in (0,1], n_keep in [1,Bk], sm_scale > 0, stages in 1..7";
+    case BSA_ERR_RANGE: return "threshold / keep ratio must lie in (0,1], n_keep in [1,Bk], sm_scale > 0, eps > 0 and normal, theta > 0, all finite, stages in 1..7";
     case BSA_ERR_CAPACITY: return "index buffer smaller than rows*N";
     case BSA_ERR_DTYPE: return "dtype must be BSA_F32 or BSA_BF16";
     case BSA_ERR_LAUNCH: return "HIP launch error";
@@ -352,7 +352,7 @@ static int rope_args(const bsa_shape_t* shape, const bsa_rope_t* rope, const flo
     if (!table) return BSA_ERR_NULL;
     if (!aligned8(table)) return BSA_ERR_STRIDE;
   }
-  if (!(eps > 0.f) || !std::isfinite(eps)) return BSA_ERR_RANGE;
+  if (!(eps > 0.f) || !std::isnormal(eps)) return BSA_ERR_RANGE;  // (v_rsq_f32 takes a subnormal number for zero)
   a->table = table;
   a->eps = eps;
   return BSA_OK;
