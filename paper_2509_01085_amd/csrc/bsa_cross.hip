@@ -9,14 +9,15 @@
 //   dQ = sm_scale dS K, dK = sm_scale dS^T Q, dV = P^T dO
 //
 // Softmax statistics, sums and accumulators are fp32.  bf16: P and dS are rounded once on their way into a product, as its operands are
-// bf16; that and the result's own rounding are what the results are off by (O 2.2e-3 rms, gradients 2.4e-3 to 2.6e-3).
+// bf16; that and the result's own rounding are what the results are off by (O 2.0e-3 rms, gradients 2.3e-3 to 2.5e-3).
 //
-// What bounds them, and what they measured (512 states, 33,280 queries, 12 heads, d = 128, bf16): the forward took 131 us (105 GFLOP,
-// 0.80 PFLOP/s; a library product of 8192^3 reaches 1.4), dQ 190 (157 GFLOP, 0.83), dK and dV (bsa_cross_dkv.hip) 199 and 7 (209 GFLOP, 1.01).
-// About 30 us of the forward are the first tiles, the rows and the results, 204 MB; a further state costs 0.2 us, 1.06 PFLOP/s, where LDS reads
-// (42 us), matrix cores (42) and vector instructions (58) of two wavefronts a SIMD are in each other's way.  One query a head and
-// 20,000 states, 8 entries: 80 us, the bytes at the rate of a copy 84, and 9 to join the shares.  fp32: 118 TFLOP/s of the 154 that a
-// library product reaches (1,200 queries, 2,000 states, 48 heads: 501, 835 and 973 us).
+// What bounds them, and what they measured (512 states, 33,280 queries, 12 heads, d = 128, bf16): the forward took 137 us (105 GFLOP,
+// 0.76 PFLOP/s; a library product of 8192^3 reaches 1.4), dQ 186 (157 GFLOP, 0.84), dK and dV (bsa_cross_dkv.hip) 195 and 7 for the join (209
+// GFLOP, 1.04 with it).  About 30 us of the forward are the first tiles, the rows and the results, 204 MB; a further state costs 0.21 us, 0.97
+// PFLOP/s, where LDS reads (42 us), matrix cores (42) and vector instructions (66) of two wavefronts a SIMD are in each other's way.  One query
+// a head and 12,134 of 20,000 states in the mean, 8 entries: 80 us, the bytes at the rate of a copy 85, and 9 to join the shares.  fp32: 118
+// TFLOP/s of the 154 that a library product reaches (1,200 queries, 2,000 states, 48 heads: 500, 832 and 972 us).  More than 128 channels are
+// far from that: 6 heads of 256, 503, 825 and 1,018 us for the same operations.
 #include <algorithm>
 
 #include "bsa_cross.h"

@@ -11,8 +11,8 @@
 // constant.  The query tiles of all units are dealt out in equal shares: 96 units (512 keys, 12 heads) of 1,040 tiles
 // (33,280 tokens) have 256 workgroups walk 390 tiles each.
 //
-// What bounds it: the matrix cores (42 % of the time busy), and beside them the exponentials and the LDS reads: there 199 us, 1.05 PFLOP/s,
-// and 7 to join the shares.  See bsa_attn_dkv.hip for the waits that inline assembly needs.
+// What bounds it: the matrix cores (42 % of the time busy), and beside them the exponentials and the LDS reads: there 195 us, 1.07 PFLOP/s,
+// and 7 to join the shares (1.04 with them).  See bsa_attn_dkv.hip for the waits that inline assembly needs.
 #include <algorithm>
 
 #include "bsa_cross.h"

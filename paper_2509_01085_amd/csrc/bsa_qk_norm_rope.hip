@@ -12,8 +12,8 @@
 // now 170).
 //
 // Measured there: forward 117 us for 614 MB (5.2 TB/s), backward 170 for 818 MB (4.8); a copy reaches 4.7.  70,400 tokens, 40 heads,
-// block-major: 856 us for 4.3 GB (5.1).  d = 72 leaves seven of sixteen lanes without channels: two batch entries of 32,760 tokens, 4 heads, 50 and
-// 88 us (3.8 TB/s).
+// block-major: 857 us for 4.3 GB (5.1).  fp32: 242 and 332 us (5.1 and 4.9).  d = 72 leaves seven of sixteen lanes without channels: two batch
+// entries of 32,760 tokens, 4 heads, 44 and 80 us (5.1 and 3.8 TB/s).
 #include "bsa_common.h"
 
 namespace bsa {
