@@ -63,7 +63,7 @@ enum bsa_status {
 
 /* Strides of a tensor with a batch, a token and a head index, in elements; the channels of a head are adjacent.
  * Multiples of 16 bytes, 0 <= stride < 2^40; that of an extent of 1 counts for nothing.  Inputs may repeat (stride 0)
- * or overlap, outputs may not. */
+ * or overlap; outputs may not, nor lie on inputs (in bsa_qk_norm_rope_bwd dXq and dXk may be Xq and Xk themselves). */
 typedef struct bsa_strides {
   int64_t b, l, h;
 } bsa_strides_t;
