@@ -9,18 +9,6 @@ from test_gpu_qk_norm_rope import CASES, DEV, projection
 pytestmark = pytest.mark.gpu
 
 
-def kernels_of(f):
-    """Names of the library's kernels that f launches."""
-    from torch.profiler import ProfilerActivity, profile
-
-    f()
-    torch.cuda.synchronize()
-    with profile(activities=[ProfilerActivity.CUDA, ProfilerActivity.CPU]) as p:
-        f()
-        torch.cuda.synchronize()
-    return {k.key for k in p.key_averages() if "bsa::" in k.key}
-
-
 @pytest.mark.parametrize("weights", (True, False))
 @pytest.mark.parametrize("name", ("block_major", "tiny_halves", "one_token"))
 def test_gradients_of_weights_are_left_out(name, weights):
@@ -39,11 +27,14 @@ def test_gradients_of_weights_are_left_out(name, weights):
     assert one[3] is None and one[4] is mine and torch.equal(mine, every[4]) and torch.equal(one[0], every[0])
 
 
-def test_without_them_there_is_no_launch_for_their_sums():
+def test_without_them_no_sums_are_left():
     shp, rope, lay = CASES["block_major"]
     gen = torch.Generator().manual_seed(82)
     (Xq, Xk, _), _ = projection(shp, lay, gen)
     dY = [torch.randn((shp.B, shp.H, shp.L, shp.d), generator=gen).to(shp.torch_dtype).to(DEV) for _ in range(3)]
     table = B.rope_table(shp, rope)
-    sums = lambda **kw: any("rope_dw" in k for k in kernels_of(lambda: B.qk_norm_rope_bwd(shp, rope, table, Xq, Xk, *dY, **kw)))  # noqa: E731
-    assert sums() and not sums(weight_grads=False)
+    ws = torch.empty(B.qk_norm_rope_bwd_workspace_bytes(shp), dtype=torch.uint8, device=DEV)
+    for weight_grads in (False, True):  # the workgroups' shares of them are all that the workspace holds
+        ws.fill_(0x5a)
+        B.qk_norm_rope_bwd(shp, rope, table, Xq, Xk, *dY, weight_grads=weight_grads, workspace=ws)
+        assert bool((ws == 0x5a).all()) != weight_grads
